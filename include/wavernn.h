@@ -73,7 +73,11 @@ typedef enum {
   WAVERNN_E_DEVICE = 5        /* the kernel reported a failure (wavernn_device_status) */
 } wavernn_status;
 
-typedef enum { WAVERNN_F32 = 0, WAVERNN_BF16 = 1 } wavernn_dtype;
+typedef enum {
+  WAVERNN_F32 = 0,
+  WAVERNN_BF16 = 1,
+  WAVERNN_F16 = 2             /* operators on callers' tensors only, no storage of a model's weights */
+} wavernn_dtype;
 
 /* Storage of R.  BSR formats keep the blocks the mask marks (Sec. 3.2):
  * 4x4 blocks, or 16x1 blocks (16 consecutive rows of one column). */
@@ -280,6 +284,110 @@ wavernn_status wavernn_score_teacher_forced(wavernn_model* m, int32_t n_streams,
                                             const float* cond_dev, int64_t n_frames, const uint16_t* target_dev,
                                             const wavernn_state* init, float* logits_c_dev, float* logits_f_dev,
                                             float* nll_dev, void* stream);
+
+/* Teacher-forced scoring as above, but of the distributions instead of the
+ * logits: for each sample the J tokens it is made of (coarse byte, fine byte;
+ * fused 2x models: high and low nibble of the coarse byte, then of the fine one),
+ *   logp_dev, entropy_dev [n_streams][n_samples][J]: log P(token) in nats (the
+ *             NLL is minus their sum) and the entropy of its distribution,
+ *   top_logp_dev, top_idx_dev [n_streams][n_samples][J][top]: its `top` most likely
+ *             values, as wavernn_token_logprobs orders them.
+ * top in [0, 32] (16 for a fused model); logp, entropy and, with top = 0, the
+ * top pointers may be NULL.  A dense model on the multi-workgroup persistent path
+ * keeps the logits of 65,536 samples at a time; the other models those of the
+ * whole call, in a model-owned buffer (2 KiB, fused 256 bytes, per sample), grown
+ * the first time a longer call needs it.  Errors: as
+ * wavernn_score_teacher_forced. */
+wavernn_status wavernn_score_tokens(wavernn_model* m, int32_t n_streams, int64_t n_samples, const float* cond_dev,
+                                    int64_t n_frames, const uint16_t* target_dev, const wavernn_state* init, int32_t top,
+                                    float* logp_dev, float* entropy_dev, float* top_logp_dev, int32_t* top_idx_dev,
+                                    void* stream);
+
+/* ---- Operators on callers' tensors -------------------------------------------
+ * The two ends of a model over tokens, and their gradients, to the definitions
+ * that scoring and conditioning use: what a program needs that trains the label
+ * table, the normalisation or the output layers of a model this library then
+ * samples.  They need no model.  All buffers are device memory of the current
+ * device, rows are `stride` elements apart (a row's elements are adjacent), and
+ * dtype is a wavernn_dtype; any alignment to whole elements and any stride of 0
+ * .. 2^31 - 1 will do for inputs, outputs need a stride of at least the row's
+ * elements.  Arithmetic and sums are fp32, each result rounded once to its
+ * type.  Results do not depend on anything but the arguments (no sum's order is
+ * left to chance).  Outputs must not overlap inputs or each other, except
+ * where a call says so.  n = 0 rows is valid.  A workspace is the caller's, of at least the bytes that
+ * the *_workspace function returns for the same sizes (-1: sizes out of range; 0: none needed,
+ * NULL will do), 16-byte aligned; its contents are nothing to keep, and calls that may
+ * overlap in time (on two streams, or captured into graphs that run side by side) need one each.
+ * The calls can be captured into a graph.  Errors: E_INVALID, E_HIP. */
+
+/* Log probability of a given token of each of n_rows distributions, given by
+ * logits [n_rows][n_classes], with the entropy and the `top` most likely classes:
+ *   lse = log sum_j exp z_j,  logp = z_token - lse,  entropy = - sum_j p_j log p_j,
+ *   top_idx, top_logp [n_rows][top]: the classes by falling logit, the lower number first
+ *   among equal ones.
+ * tokens [n_rows] are whole numbers of token_bytes 4 or 8; a negative one marks a
+ * row of padding, which is not read: logp, entropy, lse and top_logp 0, top_idx
+ * -1.  A token of n_classes or more has logp NaN.  Masked classes (-inf) have
+ * probability 0 and add nothing to the entropy; they are ordered last.  Where every class is
+ * masked, lse, logp and top_logp are -inf and the entropy is 0.  A row with a NaN
+ * or +inf has NaN in logp, entropy, lse and top_logp, and NaN is ordered above all.
+ * tokens may be NULL if logp is; each of logp, entropy, lse, and with top = 0 top_logp and
+ * top_idx, may be NULL.  top in [0, min(32, n_classes)]. */
+#define WAVERNN_MAX_TOP 32
+int64_t wavernn_token_logprobs_workspace(int64_t n_rows, int32_t n_classes, int32_t top);
+wavernn_status wavernn_token_logprobs(int32_t dtype, const void* logits_dev, int64_t n_rows, int32_t n_classes,
+                                      int64_t row_stride, const void* tokens_dev, int32_t token_bytes, int32_t top,
+                                      float* logp_dev, float* entropy_dev, float* lse_dev, float* top_logp_dev,
+                                      int32_t* top_idx_dev, void* workspace_dev, int64_t workspace_bytes, void* stream);
+/* Its gradient: with the loss's gradients g_logp, g_entropy, g_lse [n_rows] and
+ * g_top [n_rows][top] (of top_logp), each NULL where the loss does not use it,
+ *   dlogits_j = [j = token] g_logp + sum_k [j = top_idx_k] g_top_k
+ *               + p_j (g_lse - g_logp - sum_k g_top_k) - g_entropy p_j (log p_j + entropy),
+ * p_j = exp(z_j - lse), from the forward call's lse, entropy (needed with
+ * g_entropy) and top_idx (needed with top > 0; a negative one, and its g_top, is
+ * ignored).  Rows of padding and rows whose every class is masked are zero whatever
+ * the gradients hold there; with g_logp a token of n_classes or more makes its row NaN.  dlogits
+ * is of the logits' type and may be the logits (same stride). */
+wavernn_status wavernn_token_logprobs_grad(int32_t dtype, const void* logits_dev, int64_t n_rows, int32_t n_classes,
+                                           int64_t row_stride, const void* tokens_dev, int32_t token_bytes,
+                                           const float* lse_dev, const float* entropy_dev, const float* g_logp_dev,
+                                           const float* g_entropy_dev, const float* g_lse_dev, int32_t top,
+                                           const int32_t* top_idx_dev, const float* g_top_dev, void* dlogits_dev,
+                                           int64_t dlogits_stride, void* stream);
+
+/* Rows of a table by number: out_i = scale * table[ids_i], i < n_ids, rows of
+ * `dim` elements.  ids are of id_bytes 4 or 8.  A negative number is padding, a
+ * row of zeros; a number of n_table or more gives a row of NaN.  out's type is
+ * the table's or F32.  With out_stride above dim the rows can be fields of wider
+ * ones (labels of several kinds side by side in one conditioning frame). */
+wavernn_status wavernn_embed(int32_t table_dtype, const void* table_dev, int64_t n_table, int32_t dim,
+                             int64_t table_stride, const void* ids_dev, int32_t id_bytes, int64_t n_ids, float scale,
+                             int32_t out_dtype, void* out_dev, int64_t out_stride, void* stream);
+/* The table's gradient, all of it: dtable [n_table][dim] (of dout's type or F32)
+ * = scale * the sum of the rows dout_i with ids_i = its number, zero where there is
+ * none; numbers outside the table have no part in it. */
+int64_t wavernn_embed_grad_workspace(int64_t n_ids, int32_t dim, int64_t n_table);
+wavernn_status wavernn_embed_grad(int32_t dout_dtype, const void* dout_dev, int64_t n_ids, int32_t dim,
+                                  int64_t dout_stride, const void* ids_dev, int32_t id_bytes, int64_t n_table,
+                                  float scale, int32_t out_dtype, void* dtable_dev, void* workspace_dev,
+                                  int64_t workspace_bytes, void* stream);
+
+/* Layer norm of rows of `dim` elements: y = (x - mean) rstd gamma + beta with the
+ * row's mean and rstd = 1 / sqrt(variance + eps), eps > 0.  gamma, beta [dim] are of
+ * w_dtype (x's type or F32), NULL = 1 and 0.  mean, rstd [n_rows] (NULL: not
+ * wanted) are what the gradient needs.  y may be x (same stride). */
+wavernn_status wavernn_layer_norm(int32_t dtype, const void* x_dev, int64_t n_rows, int32_t dim, int64_t x_stride,
+                                  int32_t w_dtype, const void* gamma_dev, const void* beta_dev, float eps, void* y_dev,
+                                  int64_t y_stride, float* mean_dev, float* rstd_dev, void* stream);
+/* Its gradient: dx (of x's type; may be dy or x, same stride), dgamma and dbeta
+ * [dim] fp32, summed over the rows; each NULL where not wanted.  The workspace is
+ * for dgamma and dbeta. */
+int64_t wavernn_layer_norm_grad_workspace(int64_t n_rows, int32_t dim);
+wavernn_status wavernn_layer_norm_grad(int32_t dtype, const void* dy_dev, int64_t dy_stride, const void* x_dev,
+                                       int64_t x_stride, int64_t n_rows, int32_t dim, int32_t w_dtype,
+                                       const void* gamma_dev, const float* mean_dev, const float* rstd_dev, void* dx_dev,
+                                       int64_t dx_stride, float* dgamma_dev, float* dbeta_dev, void* workspace_dev,
+                                       int64_t workspace_bytes, void* stream);
 
 /* Wait for the model's last call on `stream` and report a failure the kernel
  * flagged (a bounded wait that expired): WAVERNN_OK or WAVERNN_E_DEVICE. */

@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libwavernn.so")
 SOURCES = ["wr_small.hip", "wr_persist.hip", "wr_fused.hip", "wr_batch.hip", "wr_floor.hip", "wr_cnn.hip", "wr_score.hip",
-           "wr_host.hip"]
+           "wr_logp.hip", "wr_embed.hip", "wr_norm.hip", "wr_host.hip"]
 ARCH = os.environ.get("WAVERNN_ARCH", "gfx950")
 
 

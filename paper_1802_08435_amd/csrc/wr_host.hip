@@ -13,6 +13,8 @@
 #include "wavernn.h"
 #include "wr_args.h"
 #include "wr_layout.h"
+#include "wr_logp.h"
+#include "wr_ops.h"
 
 namespace {
 
@@ -117,6 +119,15 @@ const u64 kWaitTicks = 200000000ull;  // 2 s of the 100 MHz clock per wait
 
 }  // namespace
 
+wavernn_status wr_fail(wavernn_status s, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(s, "%s", buf);
+}
+
 struct wavernn_model {
   wavernn_config cfg;
   int device = 0;
@@ -154,6 +165,8 @@ struct wavernn_model {
   int64_t traj_cap = 0;               // rows
   uint16_t* d_so = nullptr;           // [rows] split rows of the first-layer output (NP wide)
   float* d_sz = nullptr;              // [2][rows][256] logits
+  float* d_tz = nullptr;              // [2][samples] logits of a wavernn_score_tokens call on the other paths
+  int64_t tz_cap = 0;                 // its floats
   uint16_t* d_zero = nullptr;         // 128 bytes of zeros (GEMM rows read as zero)
   int64_t so_cap = 0;                       // rows of d_so and d_sz (at most one chunk of the output layers)
   u64* trace = nullptr;
@@ -1415,6 +1428,13 @@ wavernn_status launch_fill(xw* words, int64_t n_words, hipStream_t st) {
   return WAVERNN_OK;
 }
 
+// Results of wavernn_score_tokens beyond the logits.
+struct TokenIO {
+  int32_t top;
+  float *logp, *entropy, *top_logp;
+  int32_t* top_idx;
+};
+
 struct RunIO {
   int32_t S;
   int64_t T;
@@ -1434,6 +1454,7 @@ struct RunIO {
   int64_t step0 = 0;             // subscale: the schedule steps [step0, step0 + n_steps) of the call run
   int64_t n_steps = -1;          // (-1: the whole schedule, a wavernn_sample call)
   CallScope* call = nullptr;
+  const TokenIO* tok = nullptr;  // wavernn_score_tokens
   bool pinned = false;           // batch-1 grids at their own placement, whatever else runs (wavernn_tune)
 };
 
@@ -1671,6 +1692,31 @@ wavernn_status run_persist(wavernn_model* m, const RunIO& io) {
   return WAVERNN_OK;
 }
 
+// Log probabilities, entropies and alternatives of `n` samples from their
+// logits zc, zf (256 each, or two nibbles of 16 for a fused model), results of
+// sample r0 on.
+wavernn_status token_stats(const wavernn_model* m, const TokenIO& t, const float* zc, const float* zf,
+                           const uint16_t* target, int64_t r0, int64_t n, hipStream_t st) {
+  const int J = m->fused ? 4 : 2;
+  for (int k = 0; k < 2; ++k) {
+    LogpArgs a = {};
+    a.logits = k ? zf : zc;
+    a.v = m->fused ? 16 : 256;
+    a.n = m->fused ? 2 * n : n;
+    a.stride = a.v;
+    a.tokens = target + r0;
+    a.kind = m->fused ? (k ? WR_TOK_LOW4 : WR_TOK_HIGH4) : (k ? WR_TOK_LOW : WR_TOK_HIGH);
+    a.top = t.top;
+    a.logp = t.logp ? t.logp + J * r0 : nullptr;
+    a.entropy = t.entropy ? t.entropy + J * r0 : nullptr;
+    a.top_logp = t.top ? t.top_logp + J * r0 * t.top : nullptr;
+    a.top_idx = t.top ? t.top_idx + J * r0 * t.top : nullptr;
+    const wavernn_status s = wr_logp_launch(WAVERNN_F32, a, st);
+    if (s != WAVERNN_OK) return s;
+  }
+  return WAVERNN_OK;
+}
+
 // Teacher-forced scoring of one or more utterances on the dense batch-1 plan
 // (Sec. 5's NLL; Eq. 2 with the bytes given).  One launch of the scoring
 // kernel runs the recurrence of every utterance and writes h after every step; then the output
@@ -1681,7 +1727,7 @@ wavernn_status run_score(wavernn_model* m, const RunIO& io) {
   const int Hh = m->plan.Hh, NP = m->sc_np;
   const int64_t rows = (int64_t)io.S * io.T, CH = 65536;
   const int64_t n_cb = m->cfg.cond_dim > 0 ? io.n_frames : 1;
-  const bool post = io.zc || io.zf || io.nll;
+  const bool post = io.zc || io.zf || io.nll || io.tok;
   const int64_t ch = std::min(CH, rows);   // rows of one chunk of the output layers
   // One launch for all utterances: as few per group as 8 groups allow.
   const int H = m->plan.H, Dc = m->cfg.cond_dim, NW = H / 32;
@@ -1766,6 +1812,7 @@ wavernn_status run_score(wavernn_model* m, const RunIO& io) {
       void* args[] = {&zc, &zf, &tg, &nn, &nl};
       HIPOK(hipLaunchKernel(wr_score_nll_ptr(), dim3((unsigned)((n + 3) / 4)), dim3(256), args, 0, io.st));
     }
+    if (io.tok && (st = token_stats(m, *io.tok, z[0], z[1], io.target, r0, n, io.st)) != WAVERNN_OK) return st;
   }
   return WAVERNN_OK;
 }
@@ -2225,6 +2272,43 @@ wavernn_status wavernn_score_teacher_forced(wavernn_model* m, int32_t n_streams,
   RunIO io{n_streams, n_samples, cond_dev, n_frames, 0, init, nullptr, target_dev, nullptr,
            logits_c_dev, logits_f_dev, nll_dev, (hipStream_t)stream};
   return run(m, io);
+}
+
+wavernn_status wavernn_score_tokens(wavernn_model* m, int32_t n_streams, int64_t n_samples, const float* cond_dev,
+                                    int64_t n_frames, const uint16_t* target_dev, const wavernn_state* init, int32_t top,
+                                    float* logp_dev, float* entropy_dev, float* top_logp_dev, int32_t* top_idx_dev,
+                                    void* stream) {
+  if (!m) return fail(WAVERNN_E_INVALID, "null model");
+  if (!target_dev && n_samples != 0) return fail(WAVERNN_E_INVALID, "target is null");
+  const int classes = m->fused ? 16 : 256;
+  if (top < 0 || top > WAVERNN_MAX_TOP || top > classes)
+    return fail(WAVERNN_E_INVALID, "top %d not in [0, %d]", top, std::min(WAVERNN_MAX_TOP, classes));
+  if (top > 0 && n_samples > 0 && (!top_logp_dev || !top_idx_dev))
+    return fail(WAVERNN_E_INVALID, "top_logp or top_idx is null");
+  const hipStream_t st = (hipStream_t)stream;
+  const TokenIO tok{top, logp_dev, entropy_dev, top_logp_dev, top_idx_dev};
+  RunIO io{n_streams, n_samples, cond_dev, n_frames, 0, init, nullptr, target_dev, nullptr,
+           nullptr, nullptr, nullptr, st};
+  if (m->score && m->path == PATH_PERSIST && !m->fused) {
+    io.tok = &tok;
+    return run(m, io);
+  }
+  wavernn_status s = validate_run(m, io);
+  if (s != WAVERNN_OK) return s;
+  const int64_t rows = (int64_t)n_streams * n_samples, nz = m->fused ? 32 : 256;
+  if (rows == 0) return WAVERNN_OK;
+  if (2 * rows * nz > m->tz_cap) {
+    int dev = 0;
+    HIPOK(hipGetDevice(&dev));
+    if (dev != m->device) return fail(WAVERNN_E_INVALID, "model lives on device %d, current device is %d", m->device, dev);
+    HIPOK(hipStreamSynchronize(st));
+    if ((s = m->alloc(&m->d_tz, (size_t)(2 * rows * nz) * 4)) != WAVERNN_OK) return s;
+    m->tz_cap = 2 * rows * nz;
+  }
+  io.zc = m->d_tz;
+  io.zf = m->d_tz + rows * nz;
+  if ((s = run(m, io)) != WAVERNN_OK) return s;
+  return token_stats(m, tok, io.zc, io.zf, target_dev, 0, rows, st);
 }
 
 wavernn_status wavernn_device_status(wavernn_model* m, void* stream) {

@@ -1,0 +1,69 @@
+// Shared by the operators on callers' tensors (wr_logp.hip, wr_embed.hip,
+// wr_norm.hip): element types, row access, reductions, argument checks.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <algorithm>
+
+#include "wavernn.h"
+
+// Sets wavernn_last_error and returns s (wr_host.hip).
+wavernn_status wr_fail(wavernn_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+
+#define WR_LAUNCH(kernel, grid, block, lds, stream, args)                                                      \
+  do {                                                                                                         \
+    void* argv_[] = {&args};                                                                                   \
+    hipError_t e_ = hipLaunchKernel((const void*)(kernel), dim3((unsigned)(grid)), dim3(block), argv_, (lds),   \
+                                    (hipStream_t)(stream));                                                    \
+    if (e_ != hipSuccess) return wr_fail(WAVERNN_E_HIP, "launch of " #kernel ": %s", hipGetErrorString(e_));    \
+  } while (0)
+
+// Blocks of a launch whose kernels stride over their rows: enough to fill the
+// card many times over, far below the grid limit of 2^32 - 1 threads.
+#define WR_OP_BLOCKS 65536
+
+inline bool wr_dtype_ok(int t) { return t == WAVERNN_F32 || t == WAVERNN_BF16 || t == WAVERNN_F16; }
+inline int wr_dtype_bytes(int t) { return t == WAVERNN_F32 ? 4 : 2; }
+inline bool wr_aligned(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
+
+// The sizes and pointer of one matrix of rows: n rows of `width` elements, `stride` elements apart.
+inline wavernn_status wr_check_rows(const char* name, const void* p, int dtype, int64_t n, int64_t width, int64_t stride,
+                                    bool output) {
+  if (n > 0 && !p) return wr_fail(WAVERNN_E_INVALID, "%s is null", name);
+  if (!wr_aligned(p, wr_dtype_bytes(dtype))) return wr_fail(WAVERNN_E_INVALID, "%s is not aligned to its elements", name);
+  if (stride < 0 || stride > INT32_MAX) return wr_fail(WAVERNN_E_INVALID, "%s: row stride %lld out of range", name, (long long)stride);
+  if (output && n > 1 && stride < width)
+    return wr_fail(WAVERNN_E_INVALID, "%s: row stride %lld below the row's %lld elements", name, (long long)stride, (long long)width);
+  return WAVERNN_OK;
+}
+
+// Runs `body` with T the element type of dtype t.
+#define WR_DISPATCH(t, T, ...)                                        \
+  do {                                                                \
+    if ((t) == WAVERNN_F32) { using T = float; __VA_ARGS__; }         \
+    else if ((t) == WAVERNN_BF16) { using T = __bf16; __VA_ARGS__; }  \
+    else { using T = _Float16; __VA_ARGS__; }                         \
+  } while (0)
+
+// A whole number of a list of 4- or 8-byte ones.
+__device__ __forceinline__ int64_t wr_id(const void* ids, int bytes, int64_t i) {
+  return bytes == 8 ? ((const int64_t*)ids)[i] : (int64_t)((const int32_t*)ids)[i];
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+// Sum over a block of NW waves; every thread gets it.  `s`: NW floats of LDS, free for the next use
+// once every thread has passed the next barrier.
+template <int NW>
+__device__ __forceinline__ float block_sum(float v, float* s) {
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float r = s[0];
+#pragma unroll
+  for (int i = 1; i < NW; ++i) r += s[i];
+  return r;
+}

@@ -1,0 +1,248 @@
+"""Operators on GPU tensors that need no model (``include/wavernn.h``): log
+probabilities of given tokens with entropy and top alternatives, table lookup,
+layer norm, and the gradient of each.
+
+Argument marshalling only, as in ``wavernn``.  Rows are the last dimension, whose
+elements are adjacent; the dimensions before it may be any view with one distance
+between rows (a slice of wider rows, an expanded row).  Tensors of one call are on
+one GPU, which need not be the current one; the call runs on ``stream`` (default:
+that GPU's current stream), and tensors it allocates belong to that stream.  Wrong
+shapes, types or devices raise ``ValueError`` before anything is launched.  No
+function takes part in torch's autograd: a gradient is a call of its own.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import wavernn as _w
+
+MAX_TOP = 32
+_DTYPE = {torch.float32: _w.F32, torch.bfloat16: _w.BF16, torch.float16: _w.F16}
+_ID_BYTES = {torch.int32: 4, torch.int64: 8}
+
+
+def _dtype(name, t):
+    if t.dtype not in _DTYPE:
+        raise ValueError(f"{name}: dtype {t.dtype} is not float32, bfloat16 or float16")
+    return _DTYPE[t.dtype]
+
+
+def _rows(name, t):
+    """(rows, elements of a row, elements from row to row) of t [..., width]."""
+    if t.dim() == 0:
+        raise ValueError(f"{name}: needs a last dimension of elements")
+    w = t.shape[-1]
+    if w > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    if t.dim() == 2:
+        return t.shape[0], w, t.stride(0)
+    if t.dim() == 1:
+        return 1, w, w
+    n = 1
+    for s in t.shape[:-1]:
+        n *= s
+    if n == 0 or t.is_contiguous():
+        return n, w, w
+    step, run = None, 1                    # from the last leading dimension outwards
+    for d in range(t.dim() - 2, -1, -1):
+        if t.shape[d] == 1:
+            continue
+        if step is None:
+            step = t.stride(d)
+        elif t.stride(d) != step * run:
+            raise ValueError(f"{name}: the rows are not one distance apart")
+        run *= t.shape[d]
+    return n, w, w if step is None else step
+
+
+def _plain(name, t, shape, dtypes, device):
+    """t, checked to be contiguous, of the shape, on the device and of one of the dtypes."""
+    if t.shape != shape or t.device != device or t.dtype not in dtypes or not t.is_contiguous():
+        raise ValueError(f"{name}: needs a contiguous tensor {list(shape)} on {device}, "
+                         f"{' or '.join(str(d) for d in dtypes)}; got {t.dtype} {list(t.shape)} on {t.device}"
+                         f"{'' if t.is_contiguous() else ', not contiguous'}")
+    return t
+
+
+def _result(name, out, shape, dtype, device):
+    """A new tensor, or ``out`` checked to fit; with the distance between its rows."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device), shape[-1]
+    if out.shape != shape or out.dtype != dtype or out.device != device:
+        raise ValueError(f"{name}: needs {dtype} {list(shape)} on {device}, got {out.dtype} {list(out.shape)} on {out.device}")
+    return out, _rows(name, out)[2]
+
+
+def _workspace(n_bytes, device):
+    return torch.empty(n_bytes, dtype=torch.uint8, device=device) if n_bytes > 0 else None
+
+
+def _on_gpu(fn):
+    """Runs fn(t, ..., stream) with t's GPU current and, if a stream is given, that stream."""
+    def call(t, *args, stream=None, **kw):
+        if not t.is_cuda:
+            raise ValueError(f"{fn.__name__}: tensors must be on a GPU")
+        if stream is None and t.device.index == torch.cuda.current_device():
+            return fn(t, *args, **kw)
+        if stream is not None and stream.device != t.device:
+            raise ValueError(f"{fn.__name__}: the stream is on {stream.device}, the tensors on {t.device}")
+        with torch.cuda.device(t.device), torch.cuda.stream(stream):
+            return fn(t, *args, **kw)
+    call.__name__, call.__doc__, call.__wrapped__ = fn.__name__, fn.__doc__, fn
+    return call
+
+
+_F32 = (torch.float32,)
+_I32 = (torch.int32,)
+_IDS = (torch.int64, torch.int32)
+
+
+@_on_gpu
+def token_logprobs(logits, tokens=None, top=0):
+    """Log probability of tokens [...] under logits [..., V], with the entropy, the log of the
+    sum and the ``top`` most likely classes of every distribution: a dict of logp (None
+    without tokens), entropy, lse [...], top_logp and top_idx [..., top] (None with top = 0), fp32 and
+    int32.  tokens are int64 or int32; a negative one marks a row of padding, which is
+    not read and gives 0 (top_idx -1).  Masked classes are -inf.  Edge cases and the order of
+    alternatives: include/wavernn.h, wavernn_token_logprobs."""
+    L = _w.lib()
+    dt, (n, v, stride), dev, shape = _dtype("logits", logits), _rows("logits", logits), logits.device, logits.shape[:-1]
+    if tokens is not None:
+        _plain("tokens", tokens, shape, _IDS, dev)
+    ws_bytes = L.wavernn_token_logprobs_workspace(n, v, top)
+    ws = _workspace(ws_bytes, dev)
+    new = lambda *s, dtype=torch.float32: torch.empty(*s, dtype=dtype, device=dev)
+    entropy, lse = new(shape), new(shape)
+    logp = new(shape) if tokens is not None else None
+    k = max(int(top), 0)
+    top_logp, top_idx = (new(*shape, k), new(*shape, k, dtype=torch.int32)) if k else (None, None)
+    _w._check(L.wavernn_token_logprobs(dt, _w._ptr(logits), n, v, stride, _w._ptr(tokens),
+                                       _ID_BYTES[tokens.dtype] if tokens is not None else 0, top, _w._ptr(logp),
+                                       _w._ptr(entropy), _w._ptr(lse), _w._ptr(top_logp), _w._ptr(top_idx), _w._ptr(ws),
+                                       max(ws_bytes, 0), _w._stream()))
+    return dict(logp=logp, entropy=entropy, lse=lse, top_logp=top_logp, top_idx=top_idx)
+
+
+@_on_gpu
+def token_logprobs_grad(logits, tokens, lse, entropy=None, g_logp=None, g_entropy=None, g_lse=None, top_idx=None,
+                        g_top=None, out=None):
+    """Gradient with respect to the logits of a loss whose gradients with respect to
+    token_logprobs' results are g_logp, g_entropy, g_lse [...] and g_top [..., top] (of top_logp; any
+    may be None), given the results lse, entropy (for g_entropy) and top_idx (for g_top).
+    ``out`` may be the logits themselves."""
+    L = _w.lib()
+    dt, (n, v, stride), dev, shape = _dtype("logits", logits), _rows("logits", logits), logits.device, logits.shape[:-1]
+    if tokens is not None:
+        _plain("tokens", tokens, shape, _IDS, dev)
+    for name, t in (("lse", lse), ("entropy", entropy), ("g_logp", g_logp), ("g_entropy", g_entropy), ("g_lse", g_lse)):
+        if t is not None:
+            _plain(name, t, shape, _F32, dev)
+    k = 0
+    if g_top is not None:
+        k = g_top.shape[-1] if g_top.dim() else -1
+        _plain("g_top", g_top, shape + (k,), _F32, dev)
+        if top_idx is None:
+            raise ValueError("g_top needs top_idx")
+        _plain("top_idx", top_idx, shape + (k,), _I32, dev)
+    out, out_stride = _result("out", out, logits.shape, logits.dtype, dev)
+    _w._check(L.wavernn_token_logprobs_grad(dt, _w._ptr(logits), n, v, stride, _w._ptr(tokens),
+                                            _ID_BYTES[tokens.dtype] if tokens is not None else 0, _w._ptr(lse),
+                                            _w._ptr(entropy), _w._ptr(g_logp), _w._ptr(g_entropy), _w._ptr(g_lse), k,
+                                            _w._ptr(top_idx) if k else None, _w._ptr(g_top), _w._ptr(out), out_stride,
+                                            _w._stream()))
+    return out
+
+
+def _table_dtype(name, dtype, like):
+    dtype = like if dtype is None else dtype
+    if dtype != like and dtype != torch.float32:
+        raise ValueError(f"{name}: dtype must be {like} or float32")
+    return dtype
+
+
+@_on_gpu
+def embed(table, ids, scale=1.0, dtype=None, out=None):
+    """scale * table[ids]: rows of table [V, d] for ids [...] (int64 or int32) as [..., d], of the
+    table's dtype or float32.  A negative id is padding (zeros); one of V or more gives NaN.
+    ``out`` [..., d] may be a slice of wider rows."""
+    L = _w.lib()
+    dt, dev = _dtype("table", table), table.device
+    if table.dim() != 2:
+        raise ValueError("table: needs two dimensions")
+    v, d, stride = _rows("table", table)
+    _plain("ids", ids, ids.shape, _IDS, dev)
+    dtype = _table_dtype("embed", dtype, table.dtype)
+    out, out_stride = _result("out", out, ids.shape + (d,), dtype, dev)
+    _w._check(L.wavernn_embed(dt, _w._ptr(table), v, d, stride, _w._ptr(ids), _ID_BYTES[ids.dtype], ids.numel(), scale,
+                              _DTYPE[dtype], _w._ptr(out), out_stride, _w._stream()))
+    return out
+
+
+@_on_gpu
+def embed_grad(dout, ids, n_rows, scale=1.0, dtype=torch.float32):
+    """Gradient of embed's table [n_rows, d] from dout [..., d] and ids [...]: scale times
+    the sum of dout's rows for each number, zero for numbers that do not occur; sums in fp32 in an
+    order of their own, the same every time.  dtype: float32 or dout's."""
+    L = _w.lib()
+    dt, (n, d, stride), dev = _dtype("dout", dout), _rows("dout", dout), dout.device
+    _plain("ids", ids, dout.shape[:-1], _IDS, dev)
+    dtype = _table_dtype("embed_grad", dtype, dout.dtype)
+    ws_bytes = L.wavernn_embed_grad_workspace(n, d, n_rows)
+    ws = _workspace(ws_bytes, dev)
+    out = torch.empty(max(n_rows, 0), d, dtype=dtype, device=dev)
+    _w._check(L.wavernn_embed_grad(dt, _w._ptr(dout), n, d, stride, _w._ptr(ids), _ID_BYTES[ids.dtype], n_rows, scale,
+                                   _DTYPE[dtype], _w._ptr(out), _w._ptr(ws), max(ws_bytes, 0), _w._stream()))
+    return out
+
+
+def _weight(name, w, d, t, other=None):
+    if w is None:
+        return
+    _plain(name, w, (d,), (torch.float32, t.dtype), t.device)
+    if other is not None and w.dtype != other.dtype:
+        raise ValueError("gamma and beta must be of one dtype")
+
+
+@_on_gpu
+def layer_norm(x, gamma=None, beta=None, eps=1e-5, stats=False, out=None):
+    """(x - mean) / sqrt(variance + eps) * gamma + beta over the last dimension of x [..., d], of x's
+    dtype; gamma, beta [d] of x's dtype or float32.  With ``stats`` also the rows' mean and
+    1 / sqrt(variance + eps) [...], which layer_norm_grad takes.  ``out`` may be x."""
+    L = _w.lib()
+    dt, (n, d, stride), dev = _dtype("x", x), _rows("x", x), x.device
+    _weight("gamma", gamma, d, x)
+    _weight("beta", beta, d, x, gamma)
+    w = gamma if gamma is not None else beta
+    y, y_stride = _result("out", out, x.shape, x.dtype, dev)
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) if stats else None
+    rstd = torch.empty_like(mean) if stats else None
+    _w._check(L.wavernn_layer_norm(dt, _w._ptr(x), n, d, stride, _w.F32 if w is None else _DTYPE[w.dtype], _w._ptr(gamma),
+                                   _w._ptr(beta), eps, _w._ptr(y), y_stride, _w._ptr(mean), _w._ptr(rstd), _w._stream()))
+    return (y, mean, rstd) if stats else y
+
+
+@_on_gpu
+def layer_norm_grad(dy, x, mean, rstd, gamma=None, weights=True, out=None):
+    """(dx, dgamma, dbeta) of layer_norm from dy [..., d], its x and the statistics it
+    returned; dx of x's dtype, dgamma and dbeta [d] float32 (None without ``weights``).  ``out``
+    (for dx) may be dy or x."""
+    L = _w.lib()
+    dt, (n, d, stride), dev = _dtype("x", x), _rows("x", x), x.device
+    if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != dev:
+        raise ValueError("dy must be of x's shape, dtype and device")
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _plain(name, t, x.shape[:-1], _F32, dev)
+    _weight("gamma", gamma, d, x)
+    dx, dx_stride = _result("out", out, x.shape, x.dtype, dev)
+    dgamma = dbeta = ws = None
+    ws_bytes = 0
+    if weights:
+        dgamma = torch.empty(d, dtype=torch.float32, device=dev)
+        dbeta = torch.empty(d, dtype=torch.float32, device=dev)
+        ws_bytes = L.wavernn_layer_norm_grad_workspace(n, d)
+        ws = _workspace(ws_bytes, dev)
+    _w._check(L.wavernn_layer_norm_grad(dt, _w._ptr(dy), _rows("dy", dy)[2], _w._ptr(x), stride, n, d,
+                                        _w.F32 if gamma is None else _DTYPE[gamma.dtype], _w._ptr(gamma), _w._ptr(mean),
+                                        _w._ptr(rstd), _w._ptr(dx), dx_stride, _w._ptr(dgamma), _w._ptr(dbeta),
+                                        _w._ptr(ws), max(ws_bytes, 0), _w._stream()))
+    return dx, dgamma, dbeta

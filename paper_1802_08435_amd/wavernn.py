@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libwavernn.so")
 _lib = None
 
 OK, E_INVALID, E_UNSUPPORTED, E_OOM, E_HIP, E_DEVICE = range(6)
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 R_DENSE, R_BSR_4X4, R_BSR_16X1 = 0, 1, 2
 PATHS = {0: "single-workgroup", 1: "persistent", 2: "batched", 3: "block-sparse", 4: "concurrent", 5: "fused"}
 
@@ -59,7 +59,7 @@ def lib():
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is not built; run __graft_entry__.build() (hipcc, gfx950)")
         L = ctypes.CDLL(LIB_PATH)
-        vp, i32, i64, u64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64
+        vp, i32, i64, u64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
         L.wavernn_create.restype = ctypes.c_int
         L.wavernn_create.argtypes = [ctypes.POINTER(Config), ctypes.POINTER(Weights), ctypes.POINTER(vp)]
         L.wavernn_destroy.restype = None
@@ -76,6 +76,28 @@ def lib():
         L.wavernn_schedule_steps.argtypes = [vp, i64]
         L.wavernn_score_teacher_forced.restype = ctypes.c_int
         L.wavernn_score_teacher_forced.argtypes = [vp, i32, i64, vp, i64, vp, ctypes.POINTER(State), vp, vp, vp, vp]
+        L.wavernn_score_tokens.restype = ctypes.c_int
+        L.wavernn_score_tokens.argtypes = [vp, i32, i64, vp, i64, vp, ctypes.POINTER(State), i32, vp, vp, vp, vp, vp]
+        L.wavernn_token_logprobs_workspace.restype = i64
+        L.wavernn_token_logprobs_workspace.argtypes = [i64, i32, i32]
+        L.wavernn_token_logprobs.restype = ctypes.c_int
+        L.wavernn_token_logprobs.argtypes = [i32, vp, i64, i32, i64, vp, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.wavernn_token_logprobs_grad.restype = ctypes.c_int
+        L.wavernn_token_logprobs_grad.argtypes = [i32, vp, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp,
+                                                  i64, vp]
+        L.wavernn_embed.restype = ctypes.c_int
+        L.wavernn_embed.argtypes = [i32, vp, i64, i32, i64, vp, i32, i64, f32, i32, vp, i64, vp]
+        L.wavernn_embed_grad_workspace.restype = i64
+        L.wavernn_embed_grad_workspace.argtypes = [i64, i32, i64]
+        L.wavernn_embed_grad.restype = ctypes.c_int
+        L.wavernn_embed_grad.argtypes = [i32, vp, i64, i32, i64, vp, i32, i64, f32, i32, vp, vp, i64, vp]
+        L.wavernn_layer_norm.restype = ctypes.c_int
+        L.wavernn_layer_norm.argtypes = [i32, vp, i64, i32, i64, i32, vp, vp, f32, vp, i64, vp, vp, vp]
+        L.wavernn_layer_norm_grad_workspace.restype = i64
+        L.wavernn_layer_norm_grad_workspace.argtypes = [i64, i32]
+        L.wavernn_layer_norm_grad.restype = ctypes.c_int
+        L.wavernn_layer_norm_grad.argtypes = [i32, vp, i64, vp, i64, i64, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, i64,
+                                              vp]
         L.wavernn_device_status.restype = ctypes.c_int
         L.wavernn_device_status.argtypes = [vp, vp]
         L.wavernn_debug_uniforms.restype = ctypes.c_int
@@ -129,7 +151,11 @@ class Model:
     'dense', 'bsr4x4' or 'bsr16x1'.  A Fused Subscale 2x model (``fused`` true) has B = 2, F, I [3][H][6],
     O1 [4][Q][Q], b1 [4][Q], O2 [4][2][16][Q], b2 [4][2][16] and no O3, b3, O4, b4.  A subscale model
     with a future horizon may carry ``cnn``: the conditioning CNN's arrays (Win, bin, Wc, bc, Wo, bo,
-    Wp, bp; include/wavernn.h's wavernn_ctx_cnn), which replaces the window context."""
+    Wp, bp; include/wavernn.h's wavernn_ctx_cnn), which replaces the window context.
+
+    Optional front end that makes the conditioning frames (``frames``): ``E`` [n_labels][d] is a table
+    of label embeddings, scaled by ``E_scale`` (1), a frame's cond_dim / d labels side by side;
+    ``ln_g``, ``ln_b`` [cond_dim] normalise each frame (layer norm, ``ln_eps`` 1e-5)."""
 
     def __init__(self, w: dict, dtype: str = "bf16", r_format: str = "dense", max_streams: int = 1):
         L = lib()
@@ -162,6 +188,79 @@ class Model:
         _check(L.wavernn_create(ctypes.byref(cfg), ctypes.byref(ws), ctypes.byref(h)))
         self._h = h
         self.max_streams = max_streams
+        self._front(w)
+
+    def _front(self, w: dict):
+        import torch
+        up = lambda k: None if w.get(k) is None else torch.from_numpy(_f32(w[k])).cuda()
+        E, g, b = up("E"), up("ln_g"), up("ln_b")
+        if (E is not None or g is not None or b is not None) and self.cond_dim == 0:
+            raise ValueError("E, ln_g and ln_b need a model with conditioning (Wc)")
+        if E is not None and (E.dim() != 2 or E.shape[1] < 1 or self.cond_dim % E.shape[1]):
+            raise ValueError(f"E must be [n_labels][d] with d a divisor of cond_dim {self.cond_dim}")
+        for k, v in (("ln_g", g), ("ln_b", b)):
+            if v is not None and tuple(v.shape) != (self.cond_dim,):
+                raise ValueError(f"{k} must be [cond_dim] = [{self.cond_dim}]")
+        self.E, self.E_scale = E, float(w.get("E_scale", 1.0))
+        self.ln_g, self.ln_b, self.ln_eps = g, b, float(w.get("ln_eps", 1e-5))
+
+    def _embedded(self, x, stream):
+        """Rows [S][n_frames][cond_dim] before the layer norm, of labels or as given."""
+        from . import ops
+        if x.dtype.is_floating_point:
+            if x.dim() != 3 or x.shape[2] != self.cond_dim:
+                raise ValueError(f"features must be [S][n_frames][{self.cond_dim}], got {list(x.shape)}")
+            return x
+        if self.E is None:
+            raise ValueError("labels need a model with a label table (E)")
+        d = self.E.shape[1]
+        fields = self.cond_dim // d
+        if x.dim() == 2:
+            x = x.unsqueeze(-1)
+        if x.dim() != 3 or x.shape[2] != fields:
+            raise ValueError(f"labels must be [S][n_frames][{fields}], got {list(x.shape)}")
+        return ops.embed(self.E, x, scale=self.E_scale, stream=stream).view(x.shape[0], x.shape[1], self.cond_dim)
+
+    def frames(self, x, stream=None):
+        """Conditioning frames [S][n_frames][cond_dim] fp32, as sample and score take them, through the
+        model's front end: x holds labels [S][n_frames][cond_dim / d] (int64 or int32; [S][n_frames] where that
+        is 1; negative: none) or features [S][n_frames][cond_dim] fp32, which are only normalised."""
+        from . import ops
+        x = self._embedded(x, stream)
+        if self.ln_g is None and self.ln_b is None:
+            return x
+        return ops.layer_norm(x, self.ln_g, self.ln_b, eps=self.ln_eps, stream=stream)
+
+    def frames_grad(self, x, dframes, stream=None):
+        """Gradients of the front end's parameters from dframes, the loss's gradient with respect to
+        frames(x): a dict of E, ln_g, ln_b (None where the model has none or x are features)
+        and x (with respect to features; None for labels)."""
+        from . import ops
+        labels = None if x.dtype.is_floating_point else x
+        grads = dict(E=None, ln_g=None, ln_b=None, x=None)
+        d = dframes
+        if self.ln_g is not None or self.ln_b is not None:
+            rows = self._embedded(x, stream)
+            _, mean, rstd = ops.layer_norm(rows, self.ln_g, self.ln_b, eps=self.ln_eps, stats=True, stream=stream)
+            d, dg, db = ops.layer_norm_grad(dframes, rows, mean, rstd, self.ln_g, stream=stream)
+            grads["ln_g"] = None if self.ln_g is None else dg
+            grads["ln_b"] = None if self.ln_b is None else db
+        if labels is None:
+            grads["x"] = d
+        else:
+            if self.E is None:
+                raise ValueError("labels need a model with a label table (E)")
+            labels = labels.unsqueeze(-1) if labels.dim() == 2 else labels
+            grads["E"] = ops.embed_grad(d.view(*labels.shape, self.E.shape[1]), labels, self.E.shape[0],
+                                        scale=self.E_scale, stream=stream)
+        return grads
+
+    def _cond(self, cond, labels, stream):
+        if labels is None:
+            return cond
+        if cond is not None:
+            raise ValueError("cond and labels given: one of the two")
+        return self.frames(labels, stream)
 
     def close(self):
         if getattr(self, "_h", None):
@@ -200,12 +299,17 @@ class Model:
                     f=torch.zeros(n_streams * self.B, dtype=torch.uint8, device=d), t0=0)
 
     def sample(self, n_samples: int, cond=None, seed: int = 1, n_streams: int = 1, init=None, final=None,
-               out=None, stream=None, noalloc: bool = False):
+               out=None, stream=None, noalloc: bool = False, labels=None):
         """Draw n_samples per utterance; returns the [n_streams][n_samples] uint16 tensor.
+        ``labels`` in place of ``cond``: the frames are made from them by the model's front end (``frames``),
+        here and wherever both are taken.
         ``final`` (a dict from new_state) receives the state after the last sample.
         ``noalloc``: call wavernn_sample_noalloc (the library's per-device workspace,
         no device allocation; ``out`` must then be given)."""
         import torch
+        if noalloc and labels is not None:
+            raise ValueError("sample(noalloc=True) takes frames (cond), not labels")
+        cond = self._cond(cond, labels, stream)
         if out is None:
             if noalloc:
                 raise ValueError("sample(noalloc=True) needs a preallocated out tensor")
@@ -225,13 +329,14 @@ class Model:
         return int(lib().wavernn_schedule_steps(self._h, n_samples))
 
     def sample_steps(self, out, step0: int, n_steps: int, cond=None, seed: int = 1, init=None, final=None,
-                     stream=None):
+                     stream=None, labels=None):
         """Run steps [step0, step0 + n_steps) of the schedule of a subscale call
         whose whole utterances are out [S][n_samples] (uint16, holding every
         sample earlier steps made); init: the state after step0 - 1 (a dict from
         new_state, required when step0 > 0); final receives the state after the
         last step (include/wavernn.h, wavernn_sample_steps)."""
         S, n_samples = out.shape
+        cond = self._cond(cond, labels, stream)
         n_frames = 0 if cond is None else cond.shape[1]
         si, sf = self._state(init), self._state(final)
         _check(lib().wavernn_sample_steps(self._h, S, n_samples, _ptr(cond), n_frames, seed, step0, n_steps,
@@ -239,11 +344,12 @@ class Model:
                                           None if sf is None else ctypes.byref(sf), _stream(stream)))
         return out
 
-    def score(self, target, cond=None, init=None, logits: bool = True, nll: bool = True, stream=None):
+    def score(self, target, cond=None, init=None, logits: bool = True, nll: bool = True, stream=None, labels=None):
         """Teacher-forced logits [S][T][256] x2 (fused: [S][T][32]) and NLL [S][T] (nats) on target [S][T] uint16."""
         import torch
         S, T = target.shape
         nz = 32 if self.fused else 256
+        cond = self._cond(cond, labels, stream)
         zc = torch.empty(S, T, nz, device="cuda") if logits else None
         zf = torch.empty(S, T, nz, device="cuda") if logits else None
         nl = torch.empty(S, T, device="cuda") if nll else None
@@ -253,6 +359,25 @@ class Model:
                                                   None if si is None else ctypes.byref(si),
                                                   _ptr(zc), _ptr(zf), _ptr(nl), _stream(stream)))
         return dict(zc=zc, zf=zf, nll=nl)
+
+    def score_tokens(self, target, cond=None, init=None, top: int = 0, stream=None, labels=None):
+        """Teacher-forced scoring of target [S][T] uint16 by its distributions instead of their logits:
+        a dict of logp and entropy [S][T][J] (J = 2: coarse and fine byte; fused: 4, the high and
+        low nibble of each) and, with top > 0, top_logp and top_idx [S][T][J][top] (else None)."""
+        import torch
+        S, T = target.shape
+        J = 4 if self.fused else 2
+        cond = self._cond(cond, labels, stream)
+        logp, entropy = (torch.empty(S, T, J, device="cuda") for _ in range(2))
+        k = max(int(top), 0)
+        top_logp = torch.empty(S, T, J, k, device="cuda") if k else None
+        top_idx = torch.empty(S, T, J, k, dtype=torch.int32, device="cuda") if k else None
+        n_frames = 0 if cond is None else cond.shape[1]
+        si = self._state(init)
+        _check(lib().wavernn_score_tokens(self._h, S, T, _ptr(cond), n_frames, _ptr(target),
+                                          None if si is None else ctypes.byref(si), top, _ptr(logp), _ptr(entropy),
+                                          _ptr(top_logp), _ptr(top_idx), _stream(stream)))
+        return dict(logp=logp, entropy=entropy, top_logp=top_logp, top_idx=top_idx)
 
     def ctx_cnn(self, seq, stream=None):
         """Conditioning CNN over whole utterances seq [S][N] uint16: tensor [S][B][N/B][Dx]."""

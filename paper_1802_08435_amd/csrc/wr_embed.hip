@@ -29,43 +29,419 @@ __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
   }
 }
 
+// ---- the table's gradient ----------------------------------------------------
+// The positions are sorted by number (stably, so by position within a number)
+// and each run of one number is summed: nothing is added atomically, so the
+// result is the same every time.  Padding and numbers outside the table sort
+// as number n_table, behind all others.
+//
+// Sort: least significant digit first, digits of up to 9 bits (so 2 passes to
+// 262,143 rows, 1 to 511).  A wave ranks 64 numbers at a time: the lanes that
+// hold the same digit find each other by ballots, and the wave's count of that
+// digit, in LDS, is the base of their ranks.  Up to 4,096 ids one block does all
+// passes in LDS; more take two launches a pass (digit counts of every tile, then the
+// scatter), tiles of SORT_TILE ids, at most 256 tiles.
+//
+// Sum: chunks of EG_CHUNK sorted positions, one group of threads a chunk, each
+// thread one vector of columns, EG_AHEAD rows in flight.  A run inside a chunk is
+// written to the table; the parts of a run that crosses chunks go to the
+// workspace (slot 0: the chunk's beginning, slot 1: its end), and the third launch
+// adds them in chunk order.  Blocks behind the chunks' clear the rows of absent numbers.
+#define SORT_THREADS 1024
+#define SORT_WAVES 16
+#define SORT_BITS 9
+#define SORT_BINS 512
+#define SORT_SMALL 4096
+#define SORT_TILE 2048
+#define SORT_TILES 256
+#define EG_CHUNK 32
+#define EG_AHEAD 8
+
 struct EmbedGradArgs {
   const void* dout;
-  int64_t n, dout_stride;
-  int dim;
+  int64_t dout_stride;
+  int n, dim;
   const void* ids;
   int id_bytes;
-  int64_t v;
+  int v;
   float scale;
   void* dtable;
+  int passes, bits;             // of the sort
+  int tiles, tile;              // of the sort's launches; ids of a tile (a multiple of SORT_TILE)
+  uint32_t *key[2], *pos[2];    // [n] each; [1] absent with n <= SORT_SMALL
+  uint32_t* hist;               // [tiles][SORT_BINS]
+  int src, shift;               // of one pass: buffer read (-1: the ids), digit's lowest bit
+  const uint32_t *skey, *spos;  // sorted
+  float* part;                  // [chunks][2][dim]
+  int chunks, row_threads;      // row_threads: threads on a row (256 / row_threads chunks a block)
+  int chunk_blocks, clear_rows; // blocks of the sum on chunks; rows that each block behind them clears
 };
 
-// One block a row of the table: it looks for the row's number among all ids.
-template <class T, class U>
-__global__ __launch_bounds__(256) void wr_embed_grad_kernel(EmbedGradArgs a) {
-  __shared__ int64_t found[256];
-  __shared__ int count;
-  const int tid = threadIdx.x;
-  for (int64_t v = blockIdx.x; v < a.v; v += gridDim.x)
-    for (int c0 = 0; c0 < a.dim; c0 += 256) {
-      float acc = 0.0f;
-      for (int64_t i0 = 0; i0 < a.n; i0 += 256) {
-        const bool hit = i0 + tid < a.n && wr_id(a.ids, a.id_bytes, i0 + tid) == v;
-        __syncthreads();
-        found[tid] = hit;
-        __syncthreads();
-        if (tid == 0) {
-          int k = 0;
-          for (int j = 0; j < 256; ++j)
-            if (found[j]) found[k++] = i0 + j;
-          count = k;
-        }
-        __syncthreads();
-        if (c0 + tid < a.dim)
-          for (int k = 0; k < count; ++k) acc += (float)((const T*)a.dout)[found[k] * a.dout_stride + c0 + tid];
-      }
-      if (c0 + tid < a.dim) ((U*)a.dtable)[v * a.dim + c0 + tid] = (U)(acc * a.scale);
+__device__ __forceinline__ uint32_t sort_key(const EmbedGradArgs& a, int i) {
+  const int64_t id = wr_id(a.ids, a.id_bytes, i);
+  return id >= 0 && id < a.v ? (uint32_t)id : (uint32_t)a.v;
+}
+
+// Rank of this lane's digit among the lanes before it that hold the same one, and their base in the wave's
+// counts `cnt`, which grow by this round's.  Lanes without a number pass valid = false.
+__device__ __forceinline__ int wave_rank(uint16_t* cnt, int digit, int bits, bool valid) {
+  uint64_t same = __ballot(valid);
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t m = __ballot((digit >> b) & 1);
+    same &= (digit >> b) & 1 ? m : ~m;
+  }
+  const int lane = threadIdx.x & 63, below = __popcll(same & ((1ull << lane) - 1));
+  int base = 0;
+  if (valid) base = cnt[digit];
+  __builtin_amdgcn_wave_barrier();
+  if (valid && below == 0) cnt[digit] = (uint16_t)(base + __popcll(same));
+  __builtin_amdgcn_wave_barrier();
+  return base + below;
+}
+// After every wave counted its digits: cnt[w][d] becomes the count of d in the waves before w,
+// total[d] the block's.
+__device__ __forceinline__ void wave_bases(uint16_t (*cnt)[SORT_BINS], uint32_t* total) {
+  const int d = threadIdx.x;
+  if (d < SORT_BINS) {
+    int run = 0;
+#pragma unroll
+    for (int w = 0; w < SORT_WAVES; ++w) {
+      const int c = cnt[w][d];
+      cnt[w][d] = (uint16_t)run;
+      run += c;
     }
+    total[d] = run;
+  }
+}
+// x[d] becomes the sum of the x[e] with e < d.  Every thread calls it; `tmp`: 16 words.
+__device__ __forceinline__ void scan_bins(uint32_t* x, uint32_t* tmp) {
+  const int d = threadIdx.x, lane = d & 63;
+  uint32_t v = 0, s = 0;
+  if (d < SORT_BINS) {
+    v = s = x[d];
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const uint32_t t = __shfl_up(s, o, 64);
+      if (lane >= o) s += t;
+    }
+    if (lane == 63) tmp[d >> 6] = s;
+  }
+  __syncthreads();
+  if (d < SORT_BINS) {
+    for (int w = 0; w < (d >> 6); ++w) s += tmp[w];
+    x[d] = s - v;
+  }
+  __syncthreads();
+}
+
+// All passes by one block, n <= SORT_SMALL.
+__global__ __launch_bounds__(SORT_THREADS) void wr_sort_small_kernel(EmbedGradArgs a) {
+  constexpr int E = SORT_SMALL / SORT_THREADS;
+  __shared__ uint16_t cnt[SORT_WAVES][SORT_BINS];
+  __shared__ uint32_t keys[SORT_SMALL];
+  __shared__ uint16_t poss[SORT_SMALL];
+  __shared__ uint32_t base[SORT_BINS], tmp[16];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  uint32_t k[E];
+  int p[E], r[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    p[e] = wave * 64 * E + e * 64 + lane;
+    k[e] = p[e] < a.n ? sort_key(a, p[e]) : 0;
+  }
+  for (int pass = 0; pass < a.passes; ++pass) {
+    const int shift = pass * a.bits;
+    for (int i = tid; i < SORT_WAVES * SORT_BINS / 2; i += SORT_THREADS) ((uint32_t*)cnt)[i] = 0;
+    __syncthreads();
+    const uint32_t mask = (1u << a.bits) - 1;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      r[e] = wave_rank(cnt[wave], (k[e] >> shift) & mask, a.bits, wave * 64 * E + e * 64 + lane < a.n);
+    __syncthreads();
+    wave_bases(cnt, base);
+    __syncthreads();
+    scan_bins(base, tmp);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (wave * 64 * E + e * 64 + lane < a.n) {
+        const int d = (k[e] >> shift) & mask, to = base[d] + cnt[wave][d] + r[e];
+        keys[to] = k[e];
+        poss[to] = (uint16_t)p[e];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int i = wave * 64 * E + e * 64 + lane;
+      if (i < a.n) k[e] = keys[i], p[e] = poss[i];
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = wave * 64 * E + e * 64 + lane;
+    if (i < a.n) a.key[0][i] = k[e], a.pos[0][i] = (uint32_t)p[e];
+  }
+}
+
+// Counts of the pass's digits in each tile.
+__global__ __launch_bounds__(SORT_THREADS) void wr_sort_count_kernel(EmbedGradArgs a) {
+  __shared__ uint32_t h[SORT_BINS];
+  const uint32_t mask = (1u << a.bits) - 1;
+  if (threadIdx.x < SORT_BINS) h[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t i0 = (int64_t)blockIdx.x * a.tile;
+  const int64_t i1 = std::min<int64_t>(a.n, i0 + a.tile);
+  for (int64_t i = i0 + threadIdx.x; i < i1; i += SORT_THREADS)
+    atomicAdd(&h[((a.src < 0 ? sort_key(a, (int)i) : a.key[a.src][i]) >> a.shift) & mask], 1u);
+  __syncthreads();
+  if (threadIdx.x < SORT_BINS) a.hist[(int64_t)blockIdx.x * SORT_BINS + threadIdx.x] = h[threadIdx.x];
+}
+
+// One tile's numbers to their places by the pass's digit.
+__global__ __launch_bounds__(SORT_THREADS) void wr_sort_scatter_kernel(EmbedGradArgs a) {
+  constexpr int E = SORT_TILE / SORT_THREADS;
+  __shared__ uint16_t cnt[SORT_WAVES][SORT_BINS];
+  __shared__ uint32_t base[SORT_BINS], before[2][SORT_BINS], total[2][SORT_BINS], tmp[16];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const uint32_t mask = (1u << a.bits) - 1;
+  {   // this tile's first place of each digit: all smaller digits, and this one in the tiles before
+    const int d = tid & (SORT_BINS - 1), half = tid / SORT_BINS;
+    uint32_t b = 0, t = 0;
+#pragma unroll 8
+    for (int i = half; i < a.tiles; i += 2) {
+      const uint32_t c = a.hist[(int64_t)i * SORT_BINS + d];
+      t += c;
+      if (i < (int)blockIdx.x) b += c;
+    }
+    before[half][d] = b;
+    total[half][d] = t;
+  }
+  __syncthreads();
+  if (tid < SORT_BINS) base[tid] = total[0][tid] + total[1][tid];
+  __syncthreads();
+  scan_bins(base, tmp);
+  if (tid < SORT_BINS) base[tid] += before[0][tid] + before[1][tid];
+  const int dst = a.src < 0 ? 0 : 1 - a.src;
+  for (int t0 = 0; t0 < a.tile; t0 += SORT_TILE) {
+    const int64_t i0 = (int64_t)blockIdx.x * a.tile + t0;
+    if (i0 >= a.n) break;
+    for (int i = tid; i < SORT_WAVES * SORT_BINS / 2; i += SORT_THREADS) ((uint32_t*)cnt)[i] = 0;
+    __syncthreads();
+    uint32_t k[E], p[E];
+    int r[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int64_t i = i0 + wave * 64 * E + e * 64 + lane;
+      const bool in = i < a.n;
+      k[e] = in ? (a.src < 0 ? sort_key(a, (int)i) : a.key[a.src][i]) : 0;
+      p[e] = in ? (a.src < 0 ? (uint32_t)i : a.pos[a.src][i]) : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      r[e] = wave_rank(cnt[wave], (k[e] >> a.shift) & mask, a.bits, i0 + wave * 64 * E + e * 64 + lane < a.n);
+    __syncthreads();
+    wave_bases(cnt, total[0]);
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (i0 + wave * 64 * E + e * 64 + lane < a.n) {
+        const int d = (k[e] >> a.shift) & mask;
+        const uint32_t to = base[d] + cnt[wave][d] + r[e];
+        a.key[dst][to] = k[e];
+        a.pos[dst][to] = p[e];
+      }
+    __syncthreads();
+    if (tid < SORT_BINS) base[tid] += total[0][tid];
+    __syncthreads();
+  }
+}
+
+// Chunk c's columns of thread t of its row threads.
+template <class T, class U>
+__device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, int64_t c, int t) {
+  constexpr int VW = vec_of<T, U>();
+  const int rt = a.row_threads;
+  U* table = (U*)a.dtable;
+  const int64_t p0 = c * EG_CHUNK, p1 = std::min<int64_t>(a.n, p0 + EG_CHUNK);
+  const uint32_t first = a.skey[p0], last = a.skey[p1 - 1];
+  const bool from = p0 > 0 && a.skey[p0 - 1] == first, on = p1 < a.n && a.skey[p1] == last;
+  for (int col = t * VW; col < a.dim; col += rt * VW) {
+    const int count = a.dim - col;
+    float acc[VW];
+    uint32_t cur = first;
+    auto flush = [&](uint32_t id, bool at_end) {
+      if (id >= (uint32_t)a.v) return;
+      if (id == first && from) store_part<float, VW>(a.part + (2 * c) * a.dim + col, acc, count);
+      else if (at_end && on) store_part<float, VW>(a.part + (2 * c + 1) * a.dim + col, acc, count);
+      else {
+#pragma unroll
+        for (int i = 0; i < VW; ++i) acc[i] *= a.scale;
+        store_part<U, VW>(table + (int64_t)id * a.dim + col, acc, count);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < VW; ++i) acc[i] = 0.0f;
+    for (int64_t p = p0; p < p1; p += EG_AHEAD) {
+      uint32_t id[EG_AHEAD];
+      float x[EG_AHEAD][VW];
+#pragma unroll
+      for (int u = 0; u < EG_AHEAD; ++u) {
+        id[u] = p + u < p1 ? a.skey[p + u] : (uint32_t)a.v;
+        if (id[u] < (uint32_t)a.v)
+          load_part<T, VW>((const T*)a.dout + (int64_t)a.spos[p + u] * a.dout_stride + col, x[u], count);
+      }
+#pragma unroll
+      for (int u = 0; u < EG_AHEAD; ++u) {
+        if (p + u >= p1) break;
+        if (id[u] != cur) {
+          flush(cur, false);
+          cur = id[u];
+#pragma unroll
+          for (int i = 0; i < VW; ++i) acc[i] = 0.0f;
+        }
+        if (id[u] < (uint32_t)a.v)
+#pragma unroll
+          for (int i = 0; i < VW; ++i) acc[i] += x[u][i];
+      }
+    }
+    flush(cur, true);
+  }
+}
+
+template <class T, class U>
+__global__ __launch_bounds__(256) void wr_embed_sum_kernel(EmbedGradArgs a) {
+  constexpr int VW = vec_of<T, U>();
+  const int rt = a.row_threads, g = threadIdx.x / rt, t = threadIdx.x % rt;
+  U* table = (U*)a.dtable;
+  if ((int)blockIdx.x < a.chunk_blocks) {
+    for (int64_t c = (int64_t)blockIdx.x * (256 / rt) + g; c < a.chunks; c += (int64_t)a.chunk_blocks * (256 / rt))
+      sum_chunk<T, U>(a, c, t);
+    return;
+  }
+  // rows without a number
+  __shared__ int absent[256];
+  for (int64_t v0 = (int64_t)(blockIdx.x - a.chunk_blocks) * a.clear_rows; v0 < a.v;
+       v0 += (int64_t)(gridDim.x - a.chunk_blocks) * a.clear_rows) {
+    const int nr = (int)std::min<int64_t>(a.clear_rows, a.v - v0);
+    if ((int)threadIdx.x < nr) {
+      const uint32_t v = (uint32_t)(v0 + threadIdx.x);
+      int lo = 0, hi = a.n;
+      while (lo < hi) {
+        const int mid = (int)(((int64_t)lo + hi) / 2);
+        if (a.skey[mid] < v) lo = mid + 1;
+        else hi = mid;
+      }
+      absent[threadIdx.x] = lo >= a.n || a.skey[lo] != v;
+    }
+    __syncthreads();
+    float zero[VW];
+#pragma unroll
+    for (int i = 0; i < VW; ++i) zero[i] = 0.0f;
+    for (int r = g; r < nr; r += 256 / rt)
+      if (absent[r])
+        for (int col = t * VW; col < a.dim; col += rt * VW) store_part<U, VW>(table + (v0 + r) * a.dim + col, zero, a.dim - col);
+    __syncthreads();
+  }
+}
+
+// Runs that cross chunks: block c adds the parts of the run that begins in chunk c and goes on, in chunk order (each
+// group of threads every (256 / row_threads)-th part, then the groups in order).
+template <class U>
+__global__ __launch_bounds__(256) void wr_embed_join_kernel(EmbedGradArgs a) {
+  __shared__ float sums[256][4];
+  for (int64_t c = blockIdx.x; c + 1 < a.chunks; c += gridDim.x) {
+    const int64_t p0 = c * EG_CHUNK, p1 = p0 + EG_CHUNK;
+    const uint32_t id = a.skey[p1 - 1];
+    if (id >= (uint32_t)a.v || a.skey[p1] != id || (a.skey[p0] == id && p0 > 0 && a.skey[p0 - 1] == id)) continue;
+    int64_t more = 0;   // chunks after c that begin with the number
+    for (;;) {
+      const int64_t p = (c + 1 + more + threadIdx.x) * EG_CHUNK;
+      const int k = __syncthreads_count(p < a.n && a.skey[p] == id);
+      more += k;
+      if (k < 256) break;
+    }
+    const int rt = a.row_threads, groups = 256 / rt, g = threadIdx.x / rt, t = threadIdx.x % rt;
+    for (int c0 = 0; c0 < a.dim; c0 += rt * 4) {
+      const int col = c0 + t * 4, count = a.dim - col;
+      float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (count > 0)
+#pragma unroll 8
+        for (int64_t j = g; j <= more; j += groups) {
+          float x[4];
+          load_part<float, 4>(a.part + (2 * (c + j) + (j == 0)) * a.dim + col, x, count, 0.0f);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i] += x[i];
+        }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sums[threadIdx.x][i] = acc[i];
+      __syncthreads();
+      if (g == 0 && count > 0) {
+        for (int k = 1; k < groups; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i] += sums[k * rt + t][i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] *= a.scale;
+        store_part<U, 4>((U*)a.dtable + (int64_t)id * a.dim + col, acc, count);
+      }
+    }
+  }
+}
+
+// Sizes of a call and its workspace's layout; returns the workspace's bytes.
+int64_t plan_embed_grad(int64_t n, int32_t dim, int64_t v, EmbedGradArgs* a, unsigned char* ws) {
+  int bits = 1;
+  while (bits < 32 && (v >> bits)) ++bits;   // keys 0 .. v
+  a->passes = (bits + SORT_BITS - 1) / SORT_BITS;
+  a->bits = (bits + a->passes - 1) / a->passes;
+  a->tile = SORT_TILE;
+  while ((n + a->tile - 1) / a->tile > SORT_TILES) a->tile += SORT_TILE;
+  a->tiles = (int)((n + a->tile - 1) / a->tile);
+  a->chunks = (int)((n + EG_CHUNK - 1) / EG_CHUNK);
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    unsigned char* p = ws + at;
+    at += (bytes + 15) / 16 * 16;
+    return p;
+  };
+  const bool small = n <= SORT_SMALL;
+  for (int i = 0; i < (small ? 1 : 2); ++i) {
+    a->key[i] = (uint32_t*)take(4 * n);
+    a->pos[i] = (uint32_t*)take(4 * n);
+  }
+  if (!small) a->hist = (uint32_t*)take((int64_t)4 * a->tiles * SORT_BINS);
+  if (a->chunks > 1) a->part = (float*)take((int64_t)8 * a->chunks * dim);
+  return at;
+}
+
+template <class T, class U>
+wavernn_status run_embed_grad(EmbedGradArgs& a, void* stream) {
+  int last = 0;
+  if (a.n > 0 && a.n <= SORT_SMALL) {
+    WR_LAUNCH(wr_sort_small_kernel, 1, SORT_THREADS, 0, stream, a);
+  } else if (a.n > 0) {
+    for (int pass = 0; pass < a.passes; ++pass) {
+      a.src = pass == 0 ? -1 : (pass - 1) & 1;
+      a.shift = pass * a.bits;
+      WR_LAUNCH(wr_sort_count_kernel, a.tiles, SORT_THREADS, 0, stream, a);
+      WR_LAUNCH(wr_sort_scatter_kernel, a.tiles, SORT_THREADS, 0, stream, a);
+    }
+    last = (a.passes - 1) & 1;
+  }
+  a.skey = a.key[last];
+  a.spos = a.pos[last];
+  constexpr int VW = vec_of<T, U>();
+  a.row_threads = wr_row_threads((a.dim + VW - 1) / VW);
+  a.chunk_blocks = (int)std::min<int64_t>(((int64_t)a.chunks * a.row_threads + 255) / 256, 1 << 20);
+  // a block clears about 128 KiB
+  a.clear_rows = (int)std::min<int64_t>(256, std::max<int64_t>(1, 131072 / ((int64_t)a.dim * sizeof(U))));
+  const int64_t clear_blocks = std::min<int64_t>(((int64_t)a.v + a.clear_rows - 1) / a.clear_rows, 1 << 20);
+  WR_LAUNCH((wr_embed_sum_kernel<T, U>), a.chunk_blocks + clear_blocks, 256, 0, stream, a);
+  if (a.chunks > 1) {
+    a.row_threads = wr_row_threads((a.dim + 3) / 4);
+    WR_LAUNCH((wr_embed_join_kernel<U>), std::min(a.chunks - 1, 1 << 20), 256, 0, stream, a);
+  }
+  return WAVERNN_OK;
 }
 
 wavernn_status check_ids(const void* ids, int bytes, int64_t n) {
@@ -80,7 +456,7 @@ wavernn_status check_embed(int in_dtype, int out_dtype, int64_t n_table, int32_t
   if (out_dtype != in_dtype && out_dtype != WAVERNN_F32)
     return wr_fail(WAVERNN_E_INVALID, "the result's dtype must be the input's or F32");
   if (n_table < 1 || n_table > INT32_MAX) return wr_fail(WAVERNN_E_INVALID, "n_table %lld out of range", (long long)n_table);
-  if (dim < 1) return wr_fail(WAVERNN_E_INVALID, "dim %d: must be positive", dim);
+  if (dim < 1 || dim > (1 << 30)) return wr_fail(WAVERNN_E_INVALID, "dim %d not in [1, 2^30]", dim);
   return WAVERNN_OK;
 }
 
@@ -105,8 +481,9 @@ wavernn_status wavernn_embed(int32_t table_dtype, const void* table_dev, int64_t
 }
 
 int64_t wavernn_embed_grad_workspace(int64_t n_ids, int32_t dim, int64_t n_table) {
-  if (n_ids < 0 || n_ids > INT32_MAX || dim < 1 || n_table < 1 || n_table > INT32_MAX) return -1;
-  return 0;
+  if (n_ids < 0 || n_ids > INT32_MAX || dim < 1 || dim > (1 << 30) || n_table < 1 || n_table > INT32_MAX) return -1;
+  EmbedGradArgs a = {};
+  return plan_embed_grad(n_ids, dim, n_table, &a, nullptr);
 }
 
 wavernn_status wavernn_embed_grad(int32_t dout_dtype, const void* dout_dev, int64_t n_ids, int32_t dim,
@@ -121,11 +498,19 @@ wavernn_status wavernn_embed_grad(int32_t dout_dtype, const void* dout_dev, int6
   const int64_t need = wavernn_embed_grad_workspace(n_ids, dim, n_table);
   if (need > 0 && (!workspace_dev || workspace_bytes < need || !wr_aligned(workspace_dev, 16)))
     return wr_fail(WAVERNN_E_INVALID, "workspace: %lld bytes needed, 16-byte aligned", (long long)need);
-  EmbedGradArgs a{dout_dev, n_ids, dout_stride, dim, ids_dev, id_bytes, n_table, scale, dtable_dev};
-  const int64_t grid = std::min<int64_t>(n_table, WR_OP_BLOCKS);
-  WR_DISPATCH(dout_dtype, T, if (out_dtype == WAVERNN_F32) WR_LAUNCH((wr_embed_grad_kernel<T, float>), grid, 256, 0, stream, a);
-              else WR_LAUNCH((wr_embed_grad_kernel<T, T>), grid, 256, 0, stream, a));
-  return WAVERNN_OK;
+  EmbedGradArgs a = {};
+  plan_embed_grad(n_ids, dim, n_table, &a, (unsigned char*)workspace_dev);
+  a.dout = dout_dev;
+  a.dout_stride = dout_stride;
+  a.n = (int)n_ids;
+  a.dim = dim;
+  a.ids = ids_dev;
+  a.id_bytes = id_bytes;
+  a.v = (int)n_table;
+  a.scale = scale;
+  a.dtable = dtable_dev;
+  WR_DISPATCH(dout_dtype, T, return out_dtype == WAVERNN_F32 ? run_embed_grad<T, float>(a, stream)
+                                                             : run_embed_grad<T, T>(a, stream));
 }
 
 }  // extern "C"

@@ -50,6 +50,50 @@ __device__ __forceinline__ int64_t wr_id(const void* ids, int bytes, int64_t i) 
   return bytes == 8 ? ((const int64_t*)ids)[i] : (int64_t)((const int32_t*)ids)[i];
 }
 
+// N adjacent elements from or to any address aligned to an element: whole
+// vectors as one access (the hardware takes them at any alignment; at an odd
+// one an access touches two cache lines now and then), the first `count` of a
+// row's last vector one by one.
+template <class T, int N>
+__device__ __forceinline__ void load_vec(const T* p, float (&f)[N]) {
+  typedef T vec __attribute__((ext_vector_type(N)));
+  vec x;
+  __builtin_memcpy(&x, p, sizeof x);
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = (float)x[i];
+}
+template <class T, int N>
+__device__ __forceinline__ void store_vec(T* p, const float (&f)[N]) {
+  typedef T vec __attribute__((ext_vector_type(N)));
+  vec x;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = (T)f[i];
+  __builtin_memcpy(p, &x, sizeof x);
+}
+template <class T, int N>
+__device__ __forceinline__ void load_part(const T* p, float (&f)[N], int count, float rest = 0.0f) {
+  if (count >= N) return load_vec<T, N>(p, f);
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = i < count ? (float)p[i] : rest;
+}
+template <class T, int N>
+__device__ __forceinline__ void store_part(T* p, const float (&f)[N], int count) {
+  if (count >= N) return store_vec<T, N>(p, f);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (i < count) p[i] = (T)f[i];
+}
+// Elements of a 16-byte vector of the narrower of two types.
+template <class T, class U>
+constexpr int vec_of() { return 16 / (int)(sizeof(T) < sizeof(U) ? sizeof(T) : sizeof(U)); }
+
+// Threads of a block of 256 on one row of `vecs` vectors: a power of two, so that small rows share a block.
+inline int wr_row_threads(int64_t vecs) {
+  int t = 1;
+  while (t < 256 && t < vecs) t *= 2;
+  return t;
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);

@@ -16,16 +16,40 @@ struct EmbedArgs {
   float scale;
   void* out;
   int64_t out_stride;
+  int row_threads;
 };
+
+// Each group of row_threads threads copies EMBED_ROWS rows at a time, their loads in flight together.
+#define EMBED_ROWS 4
 
 template <class T, class U>
 __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
-  for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
-    const int64_t id = wr_id(a.ids, a.id_bytes, i);
-    U* o = (U*)a.out + i * a.out_stride;
-    const T* r = (const T*)a.table + (id >= 0 && id < a.v ? id : 0) * a.table_stride;
-    for (int c = threadIdx.x; c < a.dim; c += 256)
-      o[c] = id < 0 ? (U)0.0f : id >= a.v ? (U)__builtin_nanf("") : (U)((float)r[c] * a.scale);
+  constexpr int VW = vec_of<T, U>(), R = EMBED_ROWS;
+  const int rt = a.row_threads, t = threadIdx.x % rt;
+  const int64_t step = (int64_t)gridDim.x * (256 / rt) * R;
+  for (int64_t i0 = ((int64_t)blockIdx.x * (256 / rt) + threadIdx.x / rt) * R; i0 < a.n; i0 += step) {
+    int64_t id[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) id[k] = i0 + k < a.n ? wr_id(a.ids, a.id_bytes, i0 + k) : -1;
+    for (int c = t * VW; c < a.dim; c += rt * VW) {
+      const int count = a.dim - c;
+      float x[R][VW];
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        if (id[k] >= 0 && id[k] < a.v) load_part<T, VW>((const T*)a.table + id[k] * a.table_stride + c, x[k], count);
+        else
+#pragma unroll
+          for (int i = 0; i < VW; ++i) x[k][i] = 0.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        if (i0 + k >= a.n) break;
+        const float scale = id[k] < 0 ? 0.0f : id[k] < a.v ? a.scale : __builtin_nanf("");
+#pragma unroll
+        for (int i = 0; i < VW; ++i) x[k][i] *= scale;
+        store_part<U, VW>((U*)a.out + (i0 + k) * a.out_stride + c, x[k], count);
+      }
+    }
   }
 }
 
@@ -473,8 +497,10 @@ wavernn_status wavernn_embed(int32_t table_dtype, const void* table_dev, int64_t
   if ((s = wr_check_rows("table", table_dev, table_dtype, n_table, dim, table_stride, false)) != WAVERNN_OK) return s;
   if ((s = wr_check_rows("out", out_dev, out_dtype, n_ids, dim, out_stride, true)) != WAVERNN_OK) return s;
   if (n_ids == 0) return WAVERNN_OK;
-  EmbedArgs a{table_dev, n_table, table_stride, dim, ids_dev, id_bytes, n_ids, scale, out_dev, out_stride};
-  const int64_t grid = std::min<int64_t>(n_ids, WR_OP_BLOCKS);
+  EmbedArgs a{table_dev, n_table, table_stride, dim, ids_dev, id_bytes, n_ids, scale, out_dev, out_stride, 0};
+  const int vw = 16 / std::min(wr_dtype_bytes(table_dtype), wr_dtype_bytes(out_dtype));
+  a.row_threads = wr_row_threads(((int64_t)dim + vw - 1) / vw);
+  const int64_t rows = 256 / a.row_threads * EMBED_ROWS, grid = std::min<int64_t>((n_ids + rows - 1) / rows, WR_OP_BLOCKS);
   WR_DISPATCH(table_dtype, T, if (out_dtype == WAVERNN_F32) WR_LAUNCH((wr_embed_kernel<T, float>), grid, 256, 0, stream, a);
               else WR_LAUNCH((wr_embed_kernel<T, T>), grid, 256, 0, stream, a));
   return WAVERNN_OK;

@@ -3,11 +3,29 @@
 //   y = (x - m) r gamma + beta
 // and with h = (x - m) r, g = dy gamma:
 //   dx = r (g - mean g - h mean (g h)),  dgamma = sum_rows dy h,  dbeta = sum_rows dy.
-// Statistics and sums are fp32; the variance is taken about the mean in a
-// second pass, so a large mean costs no digits.
+// Statistics and sums are fp32; the variance is taken about the mean, so a
+// large mean costs no digits.
+//
+// Both are bound by memory (forward one read and one write of the rows,
+// backward two and one), so a row is read once and kept in registers between its
+// sums: RT threads a row (16 for narrow rows, so that 16 share a block, a wave,
+// or a block) with E vectors of 16 bytes each.  Blocks keep gamma and beta in registers and
+// take row after row; backward they also keep their columns' part of dgamma and dbeta,
+// which a second launch adds in the order of the blocks.  Rows past the widest
+// of these (4,096 vectors) are read from memory again for each sum.
 #include "wr_ops.h"
 
 namespace {
+
+// Vectors of a row, threads on it, vectors a thread: the first line with room.
+struct NormShape {
+  int vecs, rt, e;
+};
+constexpr NormShape kShapes[] = {{16, 16, 1},  {64, 64, 1},    {128, 64, 2},   {256, 64, 4},
+                                 {512, 256, 2}, {1024, 256, 4}, {2048, 512, 4}, {4096, 1024, 4}};
+
+#define NORM_BLOCKS 2048       // forward: eight blocks of 256 threads a CU
+#define NORM_GRAD_BLOCKS 512   // backward: parts of dgamma and dbeta
 
 struct NormArgs {
   const void* x;
@@ -20,24 +38,125 @@ struct NormArgs {
   float *mean, *rstd;
 };
 
+template <int RT>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = (RT < 64 ? RT : 64) / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+// Sums of K values over the RT threads of a row; `s` (RT > 64): [waves][K], another one for the next sum.
+template <int RT, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], float* s) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = group_sum<RT>(v[k]);
+  if constexpr (RT > 64) {
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < K; ++k) s[(threadIdx.x >> 6) * K + k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      v[k] = s[k];
+#pragma unroll
+      for (int w = 1; w < RT / 64; ++w) v[k] += s[w * K + k];
+    }
+  }
+}
+
+template <class T, class W, int RT, int E>
+__global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_kernel(NormArgs a) {
+  constexpr int VW = 16 / sizeof(T), BT = RT < 256 ? 256 : RT, G = BT / RT;
+  __shared__ float red[2][BT / 64];
+  const int t = threadIdx.x % RT;
+  const float inv_d = 1.0f / (float)a.d;
+  float ga[E][VW], be[E][VW];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int c = (e * RT + t) * VW;
+#pragma unroll
+    for (int i = 0; i < VW; ++i) ga[e][i] = 1.0f, be[e][i] = 0.0f;
+    if (a.gamma) load_part<W, VW>((const W*)a.gamma + c, ga[e], a.d - c);
+    if (a.beta) load_part<W, VW>((const W*)a.beta + c, be[e], a.d - c);
+  }
+  for (int64_t i0 = (int64_t)blockIdx.x * G; i0 < a.n; i0 += (int64_t)gridDim.x * G) {
+    const int64_t i = i0 + threadIdx.x / RT;
+    const bool on = i < a.n;   // (only the last rows of a block that shares rows; its sums stay in the group)
+    const T* x = (const T*)a.x + i * a.x_stride;
+    T* y = (T*)a.y + i * a.y_stride;
+    float v[E][VW], s[1] = {0.0f};
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = (e * RT + t) * VW;
+      load_part<T, VW>(x + c, v[e], on ? a.d - c : 0);
+#pragma unroll
+      for (int k = 0; k < VW; ++k) s[0] += v[e][k];
+    }
+    row_sums<RT, 1>(s, red[0]);
+    const float m = s[0] * inv_d;
+    s[0] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = (e * RT + t) * VW;
+#pragma unroll
+      for (int k = 0; k < VW; ++k) {
+        v[e][k] -= m;
+        if (c + k < a.d) s[0] = __builtin_fmaf(v[e][k], v[e][k], s[0]);
+      }
+    }
+    row_sums<RT, 1>(s, red[1]);
+    const float r = 1.0f / sqrtf(s[0] * inv_d + a.eps);
+    if (on) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int c = (e * RT + t) * VW;
+#pragma unroll
+        for (int k = 0; k < VW; ++k) v[e][k] = __builtin_fmaf(v[e][k] * r, ga[e][k], be[e][k]);
+        store_part<T, VW>(y + c, v[e], a.d - c);
+      }
+      if (t == 0) {
+        if (a.mean) a.mean[i] = m;
+        if (a.rstd) a.rstd[i] = r;
+      }
+    }
+  }
+}
+
+// Rows of any width, read three times.
 template <class T, class W>
-__global__ __launch_bounds__(256) void wr_norm_kernel(NormArgs a) {
-  __shared__ float red[2][4];
-  const W *gamma = (const W*)a.gamma, *beta = (const W*)a.beta;
+__global__ __launch_bounds__(1024) void wr_norm_wide_kernel(NormArgs a) {
+  constexpr int VW = 16 / sizeof(T), RT = 1024;
+  __shared__ float red[2][RT / 64];
   for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
     const T* x = (const T*)a.x + i * a.x_stride;
     T* y = (T*)a.y + i * a.y_stride;
-    float s = 0.0f;
-    for (int c = threadIdx.x; c < a.d; c += 256) s += (float)x[c];
-    const float m = block_sum<4>(s, red[0]) / (float)a.d;
-    s = 0.0f;
-    for (int c = threadIdx.x; c < a.d; c += 256) {
-      const float q = (float)x[c] - m;
-      s += q * q;
+    float s[1] = {0.0f}, v[VW];
+    for (int64_t c = threadIdx.x * VW; c < a.d; c += RT * VW) {
+      load_part<T, VW>(x + c, v, (int)(a.d - c));
+#pragma unroll
+      for (int k = 0; k < VW; ++k) s[0] += v[k];
     }
-    const float r = 1.0f / sqrtf(block_sum<4>(s, red[1]) / (float)a.d + a.eps);
-    for (int c = threadIdx.x; c < a.d; c += 256)
-      y[c] = (T)(((float)x[c] - m) * r * (gamma ? (float)gamma[c] : 1.0f) + (beta ? (float)beta[c] : 0.0f));
+    row_sums<RT, 1>(s, red[0]);
+    const float m = s[0] / (float)a.d;
+    s[0] = 0.0f;
+    for (int64_t c = threadIdx.x * VW; c < a.d; c += RT * VW) {
+      load_part<T, VW>(x + c, v, (int)(a.d - c), m);
+#pragma unroll
+      for (int k = 0; k < VW; ++k) s[0] = __builtin_fmaf(v[k] - m, v[k] - m, s[0]);
+    }
+    row_sums<RT, 1>(s, red[1]);
+    const float r = 1.0f / sqrtf(s[0] / (float)a.d + a.eps);
+    for (int64_t c = threadIdx.x * VW; c < a.d; c += RT * VW) {
+      const int count = (int)(a.d - c);
+      float ga[VW], be[VW];
+#pragma unroll
+      for (int k = 0; k < VW; ++k) ga[k] = 1.0f, be[k] = 0.0f;
+      if (a.gamma) load_part<W, VW>((const W*)a.gamma + c, ga, count);
+      if (a.beta) load_part<W, VW>((const W*)a.beta + c, be, count);
+      load_part<T, VW>(x + c, v, count);
+#pragma unroll
+      for (int k = 0; k < VW; ++k) v[k] = __builtin_fmaf((v[k] - m) * r, ga[k], be[k]);
+      store_part<T, VW>(y + c, v, count);
+    }
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[i] = m;
       if (a.rstd) a.rstd[i] = r;
@@ -54,50 +173,167 @@ struct NormGradArgs {
   void* dx;
   int64_t dx_stride;
   float *dgamma, *dbeta;
+  float* part;   // [parts][2][d]
+  int parts;
 };
 
-template <class T, class W>
-__global__ __launch_bounds__(256) void wr_norm_dx_kernel(NormGradArgs a) {
-  __shared__ float red[2][4];
-  const W* gamma = (const W*)a.gamma;
-  for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
-    const T *x = (const T*)a.x + i * a.x_stride, *dy = (const T*)a.dy + i * a.dy_stride;
-    T* dx = (T*)a.dx + i * a.dx_stride;
-    const float m = a.mean[i], r = a.rstd[i];
-    float s0 = 0.0f, s1 = 0.0f;
-    for (int c = threadIdx.x; c < a.d; c += 256) {
-      const float g = (float)dy[c] * (gamma ? (float)gamma[c] : 1.0f);
-      s0 += g;
-      s1 += g * (((float)x[c] - m) * r);
+// dx, and with WG this block's part of dgamma and dbeta.
+template <class T, class W, int RT, int E, bool WG>
+__global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_grad_kernel(NormGradArgs a) {
+  constexpr int VW = 16 / sizeof(T), BT = RT < 256 ? 256 : RT, G = BT / RT;
+  __shared__ float red[2][BT / 64 * 2];
+  const int t = threadIdx.x % RT;
+  const float inv_d = 1.0f / (float)a.d;
+  float ga[E][VW], dg[E][VW], db[E][VW];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int c = (e * RT + t) * VW;
+#pragma unroll
+    for (int k = 0; k < VW; ++k) ga[e][k] = 1.0f, dg[e][k] = db[e][k] = 0.0f;
+    if (a.gamma) load_part<W, VW>((const W*)a.gamma + c, ga[e], a.d - c);
+  }
+  int turn = 0;
+  for (int64_t i0 = (int64_t)blockIdx.x * G; i0 < a.n; i0 += (int64_t)gridDim.x * G, turn ^= 1) {
+    const int64_t i = i0 + threadIdx.x / RT;
+    const bool on = i < a.n;
+    const float m = on ? a.mean[i] : 0.0f, r = on ? a.rstd[i] : 0.0f;
+    float h[E][VW], g[E][VW], s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = (e * RT + t) * VW, count = on ? a.d - c : 0;
+      load_part<T, VW>((const T*)a.x + i * a.x_stride + c, h[e], count, m);   // (past the row: h = 0, dy = 0)
+      load_part<T, VW>((const T*)a.dy + i * a.dy_stride + c, g[e], count);
     }
-    const float m0 = block_sum<4>(s0, red[0]) / (float)a.d, m1 = block_sum<4>(s1, red[1]) / (float)a.d;
-    for (int c = threadIdx.x; c < a.d; c += 256) {
-      const float g = (float)dy[c] * (gamma ? (float)gamma[c] : 1.0f);
-      dx[c] = (T)(r * (g - m0 - ((float)x[c] - m) * r * m1));
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int k = 0; k < VW; ++k) {
+        h[e][k] = (h[e][k] - m) * r;
+        if constexpr (WG) {
+          dg[e][k] = __builtin_fmaf(g[e][k], h[e][k], dg[e][k]);
+          db[e][k] += g[e][k];
+        }
+        g[e][k] *= ga[e][k];
+        s[0] += g[e][k];
+        s[1] = __builtin_fmaf(g[e][k], h[e][k], s[1]);
+      }
+    row_sums<RT, 2>(s, red[turn]);
+    if (on && a.dx) {
+      const float m0 = s[0] * inv_d, m1 = s[1] * inv_d;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int c = (e * RT + t) * VW;
+#pragma unroll
+        for (int k = 0; k < VW; ++k) g[e][k] = r * (g[e][k] - __builtin_fmaf(h[e][k], m1, m0));
+        store_part<T, VW>((T*)a.dx + i * a.dx_stride + c, g[e], a.d - c);
+      }
+    }
+  }
+  if constexpr (WG) {
+    float* p = a.part + (int64_t)blockIdx.x * 2 * a.d;
+    if constexpr (G > 1) {   // the block's groups, in order
+      __shared__ float sum[2][VW][BT];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < VW; ++k) sum[0][k][threadIdx.x] = dg[e][k], sum[1][k][threadIdx.x] = db[e][k];
+        __syncthreads();
+        if (threadIdx.x < RT) {
+#pragma unroll
+          for (int k = 0; k < VW; ++k)
+#pragma unroll
+            for (int q = 1; q < G; ++q) {
+              dg[e][k] += sum[0][k][q * RT + t];
+              db[e][k] += sum[1][k][q * RT + t];
+            }
+        }
+      }
+      if (threadIdx.x >= RT) return;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = (e * RT + t) * VW;
+      store_part<float, VW>(p + c, dg[e], a.d - c);
+      store_part<float, VW>(p + a.d + c, db[e], a.d - c);
     }
   }
 }
 
-// 64 columns a block, four rows at a time.
-template <class T>
-__global__ __launch_bounds__(256) void wr_norm_dw_kernel(NormGradArgs a) {
-  __shared__ float red[2][256];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63);
-  float s0 = 0.0f, s1 = 0.0f;
-  if (c < a.d)
-    for (int64_t i = threadIdx.x >> 6; i < a.n; i += 4) {
-      const float dy = (float)((const T*)a.dy)[i * a.dy_stride + c];
-      s0 += dy * (((float)((const T*)a.x)[i * a.x_stride + c] - a.mean[i]) * a.rstd[i]);
-      s1 += dy;
+template <class T, class W>
+__global__ __launch_bounds__(1024) void wr_norm_grad_wide_kernel(NormGradArgs a) {
+  constexpr int VW = 16 / sizeof(T), RT = 1024;
+  __shared__ float red[2][RT / 64 * 2];
+  int turn = 0;
+  for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x, turn ^= 1) {
+    const T *x = (const T*)a.x + i * a.x_stride, *dy = (const T*)a.dy + i * a.dy_stride;
+    const float m = a.mean[i], r = a.rstd[i];
+    float s[2] = {0.0f, 0.0f}, h[VW], g[VW], ga[VW];
+    auto read = [&](int64_t c) {
+      const int count = (int)(a.d - c);
+#pragma unroll
+      for (int k = 0; k < VW; ++k) ga[k] = 1.0f;
+      if (a.gamma) load_part<W, VW>((const W*)a.gamma + c, ga, count);
+      load_part<T, VW>(x + c, h, count, m);
+      load_part<T, VW>(dy + c, g, count);
+#pragma unroll
+      for (int k = 0; k < VW; ++k) h[k] = (h[k] - m) * r, g[k] *= ga[k];
+    };
+    for (int64_t c = threadIdx.x * VW; c < a.d; c += RT * VW) {
+      read(c);
+#pragma unroll
+      for (int k = 0; k < VW; ++k) s[0] += g[k], s[1] = __builtin_fmaf(g[k], h[k], s[1]);
     }
-  red[0][threadIdx.x] = s0;
-  red[1][threadIdx.x] = s1;
+    row_sums<RT, 2>(s, red[turn]);
+    const float m0 = s[0] / (float)a.d, m1 = s[1] / (float)a.d;
+    for (int64_t c = threadIdx.x * VW; c < a.d; c += RT * VW) {
+      read(c);
+#pragma unroll
+      for (int k = 0; k < VW; ++k) g[k] = r * (g[k] - __builtin_fmaf(h[k], m1, m0));
+      store_part<T, VW>((T*)a.dx + i * a.dx_stride + c, g, (int)(a.d - c));
+    }
+  }
+}
+
+// dgamma's and dbeta's parts of wide rows: block (x, y) takes 1,024 columns of every gridDim.y-th row.
+template <class T>
+__global__ __launch_bounds__(256) void wr_norm_wide_dw_kernel(NormGradArgs a) {
+  const int64_t c = (int64_t)blockIdx.x * 1024 + threadIdx.x * 4;
+  if (c >= a.d) return;
+  const int count = (int)std::min<int64_t>(4, a.d - c);
+  float dg[4] = {}, db[4] = {}, x[4], dy[4];
+#pragma unroll 4
+  for (int64_t i = blockIdx.y; i < a.n; i += gridDim.y) {
+    const float m = a.mean[i], r = a.rstd[i];
+    load_part<T, 4>((const T*)a.x + i * a.x_stride + c, x, count, m);
+    load_part<T, 4>((const T*)a.dy + i * a.dy_stride + c, dy, count);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      dg[k] = __builtin_fmaf(dy[k], (x[k] - m) * r, dg[k]);
+      db[k] += dy[k];
+    }
+  }
+  float* p = a.part + (int64_t)blockIdx.y * 2 * a.d;
+  store_part<float, 4>(p + c, dg, count);
+  store_part<float, 4>(p + a.d + c, db, count);
+}
+
+// The parts of 64 sums added: each of 16 waves every 16th part, then the waves in order.
+__global__ __launch_bounds__(1024) void wr_norm_parts_kernel(NormGradArgs a) {
+  __shared__ float sum[16][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane, n = 2 * (int64_t)a.d;
+  float s = 0.0f;
+  if (c < n)
+#pragma unroll 8
+    for (int p = w; p < a.parts; p += 16) s += a.part[(int64_t)p * n + c];
+  sum[w][lane] = s;
   __syncthreads();
-  if (threadIdx.x < 64 && c < a.d) {
-    const float* q = red[0] + threadIdx.x;
-    if (a.dgamma) a.dgamma[c] = (q[0] + q[64]) + (q[128] + q[192]);
-    q = red[1] + threadIdx.x;
-    if (a.dbeta) a.dbeta[c] = (q[0] + q[64]) + (q[128] + q[192]);
+  if (w == 0 && c < n) {
+#pragma unroll
+    for (int q = 1; q < 16; ++q) s += sum[q][lane];
+    float* o = c < a.d ? a.dgamma : a.dbeta;
+    if (o) o[c < a.d ? c : c - a.d] = s;
   }
 }
 
@@ -106,7 +342,72 @@ wavernn_status check_norm(int dtype, int w_dtype, int64_t n, int32_t d) {
   if (w_dtype != dtype && w_dtype != WAVERNN_F32)
     return wr_fail(WAVERNN_E_INVALID, "gamma's and beta's dtype must be the rows' or F32");
   if (n < 0 || n > INT32_MAX) return wr_fail(WAVERNN_E_INVALID, "n_rows %lld out of range", (long long)n);
-  if (d < 1) return wr_fail(WAVERNN_E_INVALID, "dim %d: must be positive", d);
+  if (d < 1 || d > (1 << 30)) return wr_fail(WAVERNN_E_INVALID, "dim %d not in [1, 2^30]", d);
+  return WAVERNN_OK;
+}
+
+// Index into kShapes for rows of `vecs` vectors, or the number of shapes (wide rows).
+int norm_shape(int64_t vecs) {
+  int i = 0;
+  while (i < (int)(sizeof kShapes / sizeof kShapes[0]) && vecs > kShapes[i].vecs) ++i;
+  return i;
+}
+// Runs `body` with the shape's RT and E, `wide` if the rows are wider than all of them.
+#define NORM_SHAPE(i, RT, E, wide, ...)                              \
+  switch (i) {                                                       \
+    case 0: { constexpr int RT = kShapes[0].rt, E = kShapes[0].e; __VA_ARGS__; } break; \
+    case 1: { constexpr int RT = kShapes[1].rt, E = kShapes[1].e; __VA_ARGS__; } break; \
+    case 2: { constexpr int RT = kShapes[2].rt, E = kShapes[2].e; __VA_ARGS__; } break; \
+    case 3: { constexpr int RT = kShapes[3].rt, E = kShapes[3].e; __VA_ARGS__; } break; \
+    case 4: { constexpr int RT = kShapes[4].rt, E = kShapes[4].e; __VA_ARGS__; } break; \
+    case 5: { constexpr int RT = kShapes[5].rt, E = kShapes[5].e; __VA_ARGS__; } break; \
+    case 6: { constexpr int RT = kShapes[6].rt, E = kShapes[6].e; __VA_ARGS__; } break; \
+    case 7: { constexpr int RT = kShapes[7].rt, E = kShapes[7].e; __VA_ARGS__; } break; \
+    default: wide;                                                   \
+  }
+
+template <class T, class W>
+wavernn_status run_norm(NormArgs& a, void* stream) {
+  const int64_t vecs = ((int64_t)a.d * sizeof(T) + 15) / 16;
+  NORM_SHAPE(norm_shape(vecs), RT, E, WR_LAUNCH((wr_norm_wide_kernel<T, W>), std::min<int64_t>(a.n, NORM_BLOCKS), 1024, 0, stream, a),
+             constexpr int BT = RT < 256 ? 256 : RT;
+             const int64_t blocks = (a.n + BT / RT - 1) / (BT / RT);
+             WR_LAUNCH((wr_norm_kernel<T, W, RT, E>), std::min<int64_t>(blocks, NORM_BLOCKS), BT, 0, stream, a));
+  return WAVERNN_OK;
+}
+
+// Parts of dgamma and dbeta of a call (dtype's bytes matter to the shape): two
+// rows for each group of threads at least, so that the parts stay smaller than the rows.
+int norm_parts(int64_t n, int32_t d, int bytes) {
+  const int i = norm_shape(((int64_t)d * bytes + 15) / 16);
+  const int rt = i < (int)(sizeof kShapes / sizeof kShapes[0]) ? kShapes[i].rt : 256;
+  const int g = rt < 256 ? 256 / rt : 1;
+  return (int)std::min<int64_t>(NORM_GRAD_BLOCKS, std::max<int64_t>(1, (n + 2 * g - 1) / (2 * g)));
+}
+
+template <class T, class W>
+wavernn_status run_norm_grad(NormGradArgs& a, void* stream) {
+  const int64_t vecs = ((int64_t)a.d * sizeof(T) + 15) / 16;
+  const bool wg = a.dgamma || a.dbeta;
+  a.parts = norm_parts(a.n, a.d, sizeof(T));
+  if (a.n > 0) {
+    NORM_SHAPE(norm_shape(vecs), RT, E,
+               if (wg) {   // before dx, which may replace dy or x
+                 void* argv[] = {&a};
+                 const hipError_t e = hipLaunchKernel((const void*)wr_norm_wide_dw_kernel<T>,
+                                                      dim3((unsigned)((a.d + 1023LL) / 1024), (unsigned)a.parts), dim3(256),
+                                                      argv, 0, (hipStream_t)stream);
+                 if (e != hipSuccess) return wr_fail(WAVERNN_E_HIP, "launch of wr_norm_wide_dw_kernel: %s", hipGetErrorString(e));
+               }
+               if (a.dx) WR_LAUNCH((wr_norm_grad_wide_kernel<T, W>), std::min<int64_t>(a.n, NORM_BLOCKS), 1024, 0, stream, a),
+               constexpr int BT = RT < 256 ? 256 : RT;
+               if (wg) WR_LAUNCH((wr_norm_grad_kernel<T, W, RT, E, true>), a.parts, BT, 0, stream, a);
+               else WR_LAUNCH((wr_norm_grad_kernel<T, W, RT, E, false>),
+                              std::min<int64_t>((a.n + BT / RT - 1) / (BT / RT), NORM_BLOCKS), BT, 0, stream, a));
+  } else {
+    a.parts = 0;
+  }
+  if (wg) WR_LAUNCH(wr_norm_parts_kernel, (2 * (int64_t)a.d + 63) / 64, 1024, 0, stream, a);
   return WAVERNN_OK;
 }
 
@@ -127,15 +428,12 @@ wavernn_status wavernn_layer_norm(int32_t dtype, const void* x_dev, int64_t n_ro
   if (x_dev == y_dev && x_stride != y_stride) return wr_fail(WAVERNN_E_INVALID, "y in place of x needs the same row stride");
   if (n_rows == 0) return WAVERNN_OK;
   NormArgs a{x_dev, n_rows, x_stride, dim, gamma_dev, beta_dev, eps, y_dev, y_stride, mean_dev, rstd_dev};
-  const int64_t grid = std::min<int64_t>(n_rows, WR_OP_BLOCKS);
-  WR_DISPATCH(dtype, T, if (w_dtype == WAVERNN_F32) WR_LAUNCH((wr_norm_kernel<T, float>), grid, 256, 0, stream, a);
-              else WR_LAUNCH((wr_norm_kernel<T, T>), grid, 256, 0, stream, a));
-  return WAVERNN_OK;
+  WR_DISPATCH(dtype, T, return w_dtype == WAVERNN_F32 ? run_norm<T, float>(a, stream) : run_norm<T, T>(a, stream));
 }
 
 int64_t wavernn_layer_norm_grad_workspace(int64_t n_rows, int32_t dim) {
-  if (n_rows < 0 || n_rows > INT32_MAX || dim < 1) return -1;
-  return 0;
+  if (n_rows < 0 || n_rows > INT32_MAX || dim < 1 || dim > (1 << 30)) return -1;
+  return n_rows ? (int64_t)8 * dim * std::max(norm_parts(n_rows, dim, 2), norm_parts(n_rows, dim, 4)) : 0;
 }
 
 wavernn_status wavernn_layer_norm_grad(int32_t dtype, const void* dy_dev, int64_t dy_stride, const void* x_dev,
@@ -153,19 +451,13 @@ wavernn_status wavernn_layer_norm_grad(int32_t dtype, const void* dy_dev, int64_
     return wr_fail(WAVERNN_E_INVALID, "gamma is not aligned to its elements");
   if (dx_dev && ((dx_dev == dy_dev && dx_stride != dy_stride) || (dx_dev == x_dev && dx_stride != x_stride)))
     return wr_fail(WAVERNN_E_INVALID, "dx in place of dy or x needs the same row stride");
+  if (!dx_dev && !dgamma_dev && !dbeta_dev) return WAVERNN_OK;
   const int64_t need = dgamma_dev || dbeta_dev ? wavernn_layer_norm_grad_workspace(n_rows, dim) : 0;
   if (need > 0 && (!workspace_dev || workspace_bytes < need || !wr_aligned(workspace_dev, 16)))
     return wr_fail(WAVERNN_E_INVALID, "workspace: %lld bytes needed, 16-byte aligned", (long long)need);
   NormGradArgs a{dy_dev, x_dev, n_rows, dy_stride, x_stride, dim, gamma_dev, mean_dev, rstd_dev, dx_dev, dx_stride,
-                 dgamma_dev, dbeta_dev};
-  if (dgamma_dev || dbeta_dev)   // before dx, which may replace dy or x
-    WR_DISPATCH(dtype, T, WR_LAUNCH((wr_norm_dw_kernel<T>), (dim + 63) / 64, 256, 0, stream, a));
-  if (dx_dev && n_rows > 0) {
-    const int64_t grid = std::min<int64_t>(n_rows, WR_OP_BLOCKS);
-    WR_DISPATCH(dtype, T, if (w_dtype == WAVERNN_F32) WR_LAUNCH((wr_norm_dx_kernel<T, float>), grid, 256, 0, stream, a);
-                else WR_LAUNCH((wr_norm_dx_kernel<T, T>), grid, 256, 0, stream, a));
-  }
-  return WAVERNN_OK;
+                 dgamma_dev, dbeta_dev, (float*)workspace_dev, 0};
+  WR_DISPATCH(dtype, T, return w_dtype == WAVERNN_F32 ? run_norm_grad<T, float>(a, stream) : run_norm_grad<T, T>(a, stream));
 }
 
 }  // extern "C"

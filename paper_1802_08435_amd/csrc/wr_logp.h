@@ -25,6 +25,10 @@ struct LogpArgs {
   float *logp, *entropy, *lse;   // [n] each, or null
   float* top_logp;               // [n][top]
   int32_t* top_idx;              // [n][top]
+  // rows of several segments (set by the launch; part: the caller's workspace, or null)
+  void* part;                    // [n][splits] maximum and sums of a segment
+  unsigned long long* part_keys; // [n][splits][top] its alternatives
+  int splits, seg;               // segments of a row, classes of one
 };
 
 struct LogpGradArgs {
@@ -33,6 +37,7 @@ struct LogpGradArgs {
   const float* g_top;            // [n][f.top]
   void* dlogits;
   int64_t dstride;
+  int row_threads, splits;       // threads on a row or segment, segments of a row
 };
 
 wavernn_status wr_logp_launch(int dtype, LogpArgs& a, void* stream);

@@ -13,6 +13,9 @@
 #include "wr_logp.h"
 #include "wr_ops.h"
 
+#define LOGP_BLOCKS 2048   // eight blocks of 256 threads a CU
+#define LW_SPLITS 128      // most segments of a row
+
 namespace {
 
 // The token of a row; negative: the row is padding.
@@ -54,14 +57,8 @@ __device__ __forceinline__ float key_value(u64 k) {
 }
 __device__ __forceinline__ int key_class(u64 k) { return (int)~(uint32_t)k; }
 
-__device__ __forceinline__ u64 shfl_max(u64 v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    const u64 w = __shfl_xor(v, o, 64);
-    v = w > v ? w : v;
-  }
-  return v;
-}
+// Order of the logits alone, as top_key's upper half; 0 is below every logit.
+__device__ __forceinline__ uint32_t top_rank(float z) { return (uint32_t)(top_key(z, 0) >> 32); }
 
 // Running maximum, sum of e^(z - m) and sum of (z - m) e^(z - m).
 struct Soft {
@@ -73,9 +70,8 @@ struct Soft {
 __device__ __forceinline__ float soft_base(float m) { return m == -__builtin_inff() ? 0.0f : m; }
 // The state against a maximum m2 >= a.m.
 __device__ __forceinline__ Soft soft_at(Soft a, float m2) {
-  if (a.s == 0.0f) return Soft{m2, 0.0f, 0.0f};
   const float d = fmaxf(a.m - soft_base(m2), WR_FAR), c = fexp(d);
-  return Soft{m2, a.s * c, (a.w + d * a.s) * c};
+  return Soft{m2, a.s * c, __builtin_fmaf(d, a.s, a.w) * c};
 }
 __device__ __forceinline__ Soft soft_join(Soft a, Soft b) {
   const float m = fmaxf(a.m, b.m);
@@ -83,89 +79,463 @@ __device__ __forceinline__ Soft soft_join(Soft a, Soft b) {
   b = soft_at(b, m);
   return Soft{m, a.s + b.s, a.w + b.w};
 }
-__device__ __forceinline__ void soft_add(Soft& a, float z) {
-  if (z > a.m) a = soft_at(a, z);
-  const float d = z - soft_base(a.m), e = fexp(d);
-  a.s += e;
-  a.w += fmaxf(d, WR_FAR) * e;   // (a masked class: e = 0 and no 0 * inf)
+// One logit, z <= its maximum (base = soft_base(m)).
+__device__ __forceinline__ void soft_term(float z, float base, float& s, float& w) {
+  const float d = z - base, e = fexp(d);
+  s += e;
+  w = __builtin_fmaf(fmaxf(d, WR_FAR), e, w);
+}
+__device__ __forceinline__ float soft_lse(Soft q) { return soft_base(q.m) + logf(q.s); }
+// What is taken from a logit for its log probability: nothing where every class is masked (q.s = 0).
+__device__ __forceinline__ float soft_sub(Soft q) { return q.s == 0.0f ? 0.0f : soft_lse(q); }
+__device__ __forceinline__ float soft_entropy(Soft q) { return q.s == 0.0f ? 0.0f : logf(q.s) - q.w / q.s; }
+
+template <class T>
+__device__ __forceinline__ void put_row(const LogpArgs& a, int64_t o, int64_t t, const T* z, Soft q) {
+  if (a.logp) a.logp[o] = t < a.v ? (float)z[t] - soft_sub(q) : __builtin_nanf("");
+  if (a.entropy) a.entropy[o] = soft_entropy(q);
+  if (a.lse) a.lse[o] = soft_lse(q);
+}
+__device__ __forceinline__ void put_padding(const LogpArgs& a, int64_t o, int i) {
+  if (i == 0) {
+    if (a.logp) a.logp[o] = 0.0f;
+    if (a.entropy) a.entropy[o] = 0.0f;
+    if (a.lse) a.lse[o] = 0.0f;
+  }
+  if (i < a.top) a.top_logp[o * a.top + i] = 0.0f, a.top_idx[o * a.top + i] = -1;
 }
 
-// One block a row, any number of classes.
-template <class T>
-__global__ __launch_bounds__(256) void wr_logp_kernel(LogpArgs a) {
-  __shared__ Soft ss[4];
-  __shared__ u64 sk[4];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+// ---- a group of lanes a row ----------------------------------------------------
+// Reductions over RT = 16 lanes by rotations within a row of 16 (every lane gets the result, in the same bits, as
+// each step only exchanges the operands of a commutative operation), over 64 by joining the four rows' results.
+template <int N>
+__device__ __forceinline__ int rotate16(int v) { return __builtin_amdgcn_update_dpp(v, v, 0x120 + N, 0xf, 0xf, false); }
+template <int RT, class F>
+__device__ __forceinline__ int group_reduce(int v, F f) {
+  v = f(v, rotate16<8>(v));
+  v = f(v, rotate16<4>(v));
+  v = f(v, rotate16<2>(v));
+  v = f(v, rotate16<1>(v));
+  if constexpr (RT == 64)
+    v = f(f(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+          f(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+  return v;
+}
+template <int RT>
+__device__ __forceinline__ float group_fmax(float v) {
+  return __int_as_float(group_reduce<RT>(__float_as_int(v), [](int a, int b) {
+    return __float_as_int(fmaxf(__int_as_float(a), __int_as_float(b)));
+  }));
+}
+template <int RT>
+__device__ __forceinline__ float group_fsum(float v) {
+  return __int_as_float(group_reduce<RT>(__float_as_int(v), [](int a, int b) {
+    return __float_as_int(__int_as_float(a) + __int_as_float(b));
+  }));
+}
+template <int RT>
+__device__ __forceinline__ uint32_t group_umax(uint32_t v) {
+  return (uint32_t)group_reduce<RT>((int)v, [](int a, int b) { return (int)((uint32_t)a > (uint32_t)b ? (uint32_t)a : (uint32_t)b); });
+}
+template <int RT>
+__device__ __forceinline__ uint32_t group_umin(uint32_t v) {
+  return (uint32_t)group_reduce<RT>((int)v, [](int a, int b) { return (int)((uint32_t)a < (uint32_t)b ? (uint32_t)a : (uint32_t)b); });
+}
+
+// Rows of up to RT * E vectors of 16 bytes, in registers: class (e RT + lane) VW + k.
+// The alternatives are drawn one by one: each lane offers its best class left.
+template <class T, int RT, int E>
+__global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
+  constexpr int VW = 16 / sizeof(T), KR = (WAVERNN_MAX_TOP + RT - 1) / RT;
+  const int lane = threadIdx.x % RT;
+  const int64_t step = (int64_t)gridDim.x * (256 / RT);
+  for (int64_t row = (int64_t)blockIdx.x * (256 / RT) + threadIdx.x / RT; row < a.n; row += step) {
     const int64_t t = row_token(a, row), o = row_out(a, row);
     if (t < 0) {
-      if (tid == 0) {
-        if (a.logp) a.logp[o] = 0.0f;
-        if (a.entropy) a.entropy[o] = 0.0f;
-        if (a.lse) a.lse[o] = 0.0f;
-      }
-      if (tid < a.top) a.top_logp[o * a.top + tid] = 0.0f, a.top_idx[o * a.top + tid] = -1;
+      for (int i = lane; i == lane || i < a.top; i += RT) put_padding(a, o, i);
       continue;
     }
-    const T* z = (const T*)a.logits + row * a.stride;
+    const T* zr = (const T*)a.logits + row * a.stride;
+    float z[E][VW];
     Soft q{-__builtin_inff(), 0.0f, 0.0f};
-    for (int j = tid; j < a.v; j += 256) soft_add(q, (float)z[j]);
-    for (int d = 32; d >= 1; d >>= 1)
-      q = soft_join(q, Soft{__shfl_xor(q.m, d, 64), __shfl_xor(q.s, d, 64), __shfl_xor(q.w, d, 64)});
-    __syncthreads();   // the previous row's results are read
-    if (lane == 0) ss[wave] = q;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = (e * RT + lane) * VW;
+      load_part<T, VW>(zr + c, z[e], a.v - c, -__builtin_inff());
+#pragma unroll
+      for (int k = 0; k < VW; ++k) q.m = fmaxf(q.m, z[e][k]);
+    }
+    q.m = group_fmax<RT>(q.m);
+    const float base = soft_base(q.m);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int k = 0; k < VW; ++k) soft_term(z[e][k], base, q.s, q.w);
+    q.s = group_fsum<RT>(q.s);
+    q.w = group_fsum<RT>(q.w);
+    if (lane == 0) put_row(a, o, t, zr, q);
+    if (a.top == 0) continue;
+    uint32_t key[E][VW], best = 0, at = 0, won[KR] = {}, won_at[KR] = {};
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int k = 0; k < VW; ++k) key[e][k] = (e * RT + lane) * VW + k < a.v ? top_rank(z[e][k]) : 0;
+    auto offer = [&]() {   // the lane's best class left, the lowest among equal ones
+      best = 0, at = 0xffffffffu;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int k = 0; k < VW; ++k)
+          if (key[e][k] > best) best = key[e][k], at = (e * RT + lane) * VW + k;
+    };
+    offer();
+    for (int i = 0; i < a.top; ++i) {
+      const uint32_t m = group_umax<RT>(best), j = group_umin<RT>(best == m ? at : 0xffffffffu);
+#pragma unroll
+      for (int r = 0; r < KR; ++r)
+        if (lane + r * RT == i) won[r] = m, won_at[r] = j;
+      if (at == j) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+          for (int k = 0; k < VW; ++k)
+            if ((uint32_t)((e * RT + lane) * VW + k) == j) key[e][k] = 0;
+        offer();
+      }
+    }
+    const float sub = soft_sub(q);
+#pragma unroll
+    for (int r = 0; r < KR; ++r)
+      if (lane + r * RT < a.top) {
+        a.top_idx[o * a.top + lane + r * RT] = (int)won_at[r];
+        a.top_logp[o * a.top + lane + r * RT] = key_value((u64)won[r] << 32) - sub;
+      }
+  }
+}
+
+// ---- a block a row, or a block a segment of a row --------------------------------
+// One pass over the row, four vectors a thread in flight, with the running maximum and
+// sums of each thread; the alternatives are then looked for where they can be.  Each quad of lanes
+// keeps the largest logit it saw.  The top-th largest of the 64 quads' values, `low`, is no
+// larger than the top-th largest logit, so only quads that reach it can hold an
+// alternative: their vectors (for few alternatives a small part of the row) are read once more,
+// from cache, and the classes that reach `low` are ranked among each other.
+#define LW_U 4        // vectors in flight
+#define LW_CAP 1024   // classes ranked
+
+struct LogpShared {
+  Soft soft[4];
+  uint32_t quad[64];
+  int count, need;
+  u64 list[LW_CAP];
+  u64 wave_best[4];
+  int wave_count[4];
+  uint8_t quads[4][64];   // each wave's list of the quads to look into
+};
+
+// What is found of a row or segment: kept for the join if the row has several.
+struct LogpPart {
+  Soft q;
+  float pad;
+};
+
+// Writes alternative k (0 <= k < top) of the row or segment.
+__device__ __forceinline__ void put_top(const LogpArgs& a, int64_t o, int64_t part, int k, u64 key, float sub) {
+  if (a.splits > 1) {
+    a.part_keys[part * a.top + k] = key;
+  } else {
+    a.top_idx[o * a.top + k] = key_class(key);
+    a.top_logp[o * a.top + k] = key_value(key) - sub;
+  }
+}
+// The `top` largest of the n classes listed, in order, by counting the larger ones.
+__device__ __forceinline__ void put_ranked(const LogpArgs& a, LogpShared& sh, int n, int64_t o, int64_t part, float sub) {
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const u64 key = sh.list[i];
+    int r = 0;
+    for (int j = 0; j < n; ++j) r += sh.list[j] > key;
+    if (r < a.top) put_top(a, o, part, r, key, sub);
+  }
+}
+
+// The alternatives of classes j0 .. j0 + nj - 1, whose vectors the block's threads took in turn.
+template <class T>
+__device__ __forceinline__ void find_top(const LogpArgs& a, LogpShared& sh, const T* z0, int j0, int nj, int vecs, int64_t o,
+                                         int64_t part, float sub) {
+  constexpr int VW = 16 / sizeof(T);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  // every wave finds the top-th largest quad for itself, bit by bit
+  const uint32_t mine = sh.quad[lane];
+  uint32_t low = 0;
+  for (int b = 31; b >= 0; --b) {
+    const uint32_t tryit = low | 1u << b;
+    if (__popcll(__ballot(mine >= tryit)) >= a.top) low = tryit;
+  }
+  const u64 quads = __ballot(mine >= low && mine > 0);
+  const int nq = __popcll(quads);
+  if (quads >> lane & 1) sh.quads[wave][__popcll(quads & ((1ull << lane) - 1))] = (uint8_t)lane;
+  __builtin_amdgcn_wave_barrier();
+  // reads the vectors of those quads: thread tid takes lane tid % 4 of quad number tid / 4, and so on
+  auto scan = [&](auto&& take) {
+    const int rounds = (vecs + 255) / 256;   // vectors of a thread
+    for (int x = tid >> 2; x < nq * rounds; x += 64) {
+      const int vec = x / nq * 256 + sh.quads[wave][x % nq] * 4 + (tid & 3);
+      if (vec >= vecs) continue;
+      float z[VW];
+      const int c = vec * VW, count = nj - c;
+      load_part<T, VW>(z0 + c, z, count);
+#pragma unroll
+      for (int k = 0; k < VW; ++k)
+        if (k < count) take(z[k], j0 + c + k);
+    }
+  };
+  scan([&](float z, int j) {
+    if (top_rank(z) >= low) {
+      const int at = atomicAdd(&sh.count, 1);
+      if (at < LW_CAP) sh.list[at] = top_key(z, j);
+    }
+  });
+  __syncthreads();
+  int n = sh.count;
+  if (n <= LW_CAP) return put_ranked(a, sh, n, o, part, sub);
+  // Too many equal or close classes.  Those above `low` alone, and then the first that equal it:
+  __syncthreads();
+  if (tid == 0) sh.count = 0;
+  __syncthreads();
+  scan([&](float z, int j) {
+    if (top_rank(z) > low) {
+      const int at = atomicAdd(&sh.count, 1);
+      if (at < LW_CAP) sh.list[at] = top_key(z, j);
+    }
+  });
+  __syncthreads();
+  n = sh.count;
+  if (n <= LW_CAP) {
+    put_ranked(a, sh, n, o, part, sub);
+    int have = n;
+    for (int i0 = 0; have < a.top && i0 < vecs; i0 += 256) {
+      float z[VW];
+      const int c = (i0 + tid) * VW, count = i0 + tid < vecs ? min(nj - c, VW) : 0;
+      load_part<T, VW>(z0 + c, z, count);
+      int mineq = 0;
+#pragma unroll
+      for (int k = 0; k < VW; ++k) mineq += k < count && top_rank(z[k]) == low;
+      int before = mineq;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int x = __shfl_up(before, d, 64);
+        if (lane >= d) before += x;
+      }
+      if (lane == 63) sh.wave_count[wave] = before;
+      __syncthreads();
+      int r = have + before - mineq;
+      for (int w = 0; w < 4; ++w) {
+        if (w < wave) r += sh.wave_count[w];
+        have += sh.wave_count[w];
+      }
+#pragma unroll
+      for (int k = 0; k < VW; ++k)
+        if (k < count && top_rank(z[k]) == low) {
+          if (r < a.top) put_top(a, o, part, r, top_key(z[k], j0 + c + k), sub);
+          ++r;
+        }
+      __syncthreads();
+    }
+    return;
+  }
+  // One after another: the largest class below the last one found.
+  u64 prev = ~0ull;
+  for (int k = 0; k < a.top; ++k) {
+    u64 best = 0;
+    scan([&](float z, int j) {
+      const u64 key = top_key(z, j);
+      if (key < prev && key > best) best = key;
+    });
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+      const u64 x = __shfl_xor(best, d, 64);
+      best = x > best ? x : best;
+    }
     __syncthreads();
-    q = soft_join(soft_join(ss[0], ss[1]), soft_join(ss[2], ss[3]));
-    const float lse = soft_base(q.m) + logf(q.s);
-    if (tid == 0) {
-      if (a.logp) a.logp[o] = t < a.v ? (float)z[t] - (q.s == 0.0f ? 0.0f : lse) : __builtin_nanf("");
-      if (a.entropy) a.entropy[o] = q.s == 0.0f ? 0.0f : logf(q.s) - q.w / q.s;
-      if (a.lse) a.lse[o] = lse;
-    }
-    u64 prev = ~0ull;
-    for (int k = 0; k < a.top; ++k) {
-      u64 best = 0;
-      for (int j = tid; j < a.v; j += 256) {
-        const u64 key = top_key((float)z[j], j);
-        if (key < prev && key > best) best = key;
-      }
-      best = shfl_max(best);
-      __syncthreads();
-      if (lane == 0) sk[wave] = best;
-      __syncthreads();
-      for (int i = 0; i < 4; ++i) best = sk[i] > best ? sk[i] : best;
-      if (tid == 0) {
-        a.top_idx[o * a.top + k] = key_class(best);
-        a.top_logp[o * a.top + k] = key_value(best) - (q.s == 0.0f ? 0.0f : lse);
-      }
-      prev = best;
-    }
+    if (lane == 0) sh.wave_best[wave] = best;
+    __syncthreads();
+    for (int w = 0; w < 4; ++w) best = sh.wave_best[w] > best ? sh.wave_best[w] : best;
+    if (tid == 0) put_top(a, o, part, k, best, sub);
+    prev = best;
   }
 }
 
 template <class T>
+__global__ __launch_bounds__(256) void wr_logp_kernel(LogpArgs a) {
+  constexpr int VW = 16 / sizeof(T);
+  __shared__ LogpShared sh;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int64_t items = a.n * a.splits;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t row = a.splits > 1 ? item / a.splits : item;
+    const int64_t t = row_token(a, row), o = row_out(a, row);
+    if (t < 0) {
+      if (a.splits == 1) put_padding(a, o, tid);
+      continue;
+    }
+    const T* zr = (const T*)a.logits + row * a.stride;
+    // classes j0 .. j1 - 1 of the row, thread t's vectors t, t + 256, ... of them
+    const int j0 = a.splits > 1 ? (int)(item % a.splits) * a.seg : 0;
+    const int j1 = a.splits > 1 ? (int)std::min<int64_t>(a.v, (int64_t)j0 + a.seg) : a.v;
+    const T* z0 = zr + j0;
+    const int nj = j1 - j0, vecs = (nj + VW - 1) / VW;
+    Soft q{-__builtin_inff(), 0.0f, 0.0f};
+    for (int i = tid; i < vecs; i += 256 * LW_U) {
+      float z[LW_U][VW], m = q.m;
+#pragma unroll
+      for (int u = 0; u < LW_U; ++u) {
+        const int64_t c = (int64_t)(i + u * 256) * VW;
+        load_part<T, VW>(z0 + c, z[u], i + u * 256 < vecs ? nj - (int)c : 0, -__builtin_inff());
+      }
+#pragma unroll
+      for (int u = 0; u < LW_U; ++u)
+#pragma unroll
+        for (int k = 0; k < VW; ++k) m = fmaxf(m, z[u][k]);
+      if (m > q.m) q = soft_at(q, m);
+      const float base = soft_base(m);
+#pragma unroll
+      for (int u = 0; u < LW_U; ++u)
+#pragma unroll
+        for (int k = 0; k < VW; ++k) soft_term(z[u][k], base, q.s, q.w);
+    }
+    const float best = q.m;
+    const bool nan = q.s != q.s;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1)
+      q = soft_join(q, Soft{__shfl_xor(q.m, d, 64), __shfl_xor(q.s, d, 64), __shfl_xor(q.w, d, 64)});
+    if (lane == 0) sh.soft[wave] = q;
+    if (a.top > 0) {
+      uint32_t r = tid < vecs ? top_rank(best) : 0;
+      if (nan)   // a NaN, which comes first among the alternatives and which the maximum passes over, or +inf
+        for (int i = tid; i < vecs; i += 256)
+          for (int j = i * VW; j < min(nj, (i + 1) * VW); ++j) r = max(r, top_rank((float)z0[j]));
+      r = max(r, (uint32_t)__builtin_amdgcn_update_dpp((int)r, (int)r, 0xb1, 0xf, 0xf, false));   // quad: lanes 1 0 3 2
+      r = max(r, (uint32_t)__builtin_amdgcn_update_dpp((int)r, (int)r, 0x4e, 0xf, 0xf, false));   // quad: lanes 2 3 0 1
+      if ((lane & 3) == 0) sh.quad[tid >> 2] = r;
+      if (tid == 0) sh.count = 0;
+    }
+    __syncthreads();
+    q = soft_join(soft_join(sh.soft[0], sh.soft[1]), soft_join(sh.soft[2], sh.soft[3]));
+    if (tid == 0) {
+      if (a.splits == 1) put_row(a, o, t, zr, q);
+      else ((LogpPart*)a.part)[item].q = q;
+    }
+    if (a.top > 0) {
+      const float sub = a.splits == 1 ? soft_sub(q) : 0.0f;
+      find_top<T>(a, sh, z0, j0, nj, vecs, o, item, sub);
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the segments of each row.
+template <class T>
+__global__ __launch_bounds__(256) void wr_logp_join_kernel(LogpArgs a) {
+  __shared__ LogpShared sh;
+  const int tid = threadIdx.x, lane = tid & 63;
+  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+    const int64_t t = row_token(a, row), o = row_out(a, row);
+    if (t < 0) {
+      put_padding(a, o, tid);
+      continue;
+    }
+    const LogpPart* part = (const LogpPart*)a.part + row * a.splits;
+    Soft q{-__builtin_inff(), 0.0f, 0.0f};
+    for (int i = lane; i < a.splits; i += 64) q = soft_join(q, part[i].q);   // every wave the same
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1)
+      q = soft_join(q, Soft{__shfl_xor(q.m, d, 64), __shfl_xor(q.s, d, 64), __shfl_xor(q.w, d, 64)});
+    if (tid == 0) put_row(a, o, t, (const T*)a.logits + row * a.stride, q);
+    if (a.top == 0) continue;
+    // The segments' best classes come first: the top-th largest of them is a lower bound, reached in at
+    // most `top` segments, so at most top^2 classes are ranked.
+    const u64* keys = a.part_keys + row * a.splits * a.top;
+    if (tid < a.splits) sh.list[tid] = keys[tid * a.top];
+    if (tid == 0) sh.count = 0;
+    u64 low = 0;
+    __syncthreads();
+    if (a.splits >= a.top) {
+      if (tid < a.splits) {
+        int r = 0;
+        for (int j = 0; j < a.splits; ++j) r += sh.list[j] > sh.list[tid];
+        if (r == a.top - 1) sh.wave_best[0] = sh.list[tid];
+      }
+      __syncthreads();
+      low = sh.wave_best[0];
+    }
+    __syncthreads();
+    for (int i = tid; i < a.splits * a.top; i += 256) {
+      const u64 key = keys[i];
+      if (key >= low) sh.list[atomicAdd(&sh.count, 1)] = key;
+    }
+    __syncthreads();
+    LogpArgs b = a;
+    b.splits = 1;
+    put_ranked(b, sh, sh.count, o, 0, soft_sub(q));
+    __syncthreads();
+  }
+}
+
+// ---- gradient ----------------------------------------------------------------
+// One thread a vector, LG_U vectors in flight; rows of up to 256 LG_U vectors share
+// blocks or take one, wider ones take a block for every 256 LG_U vectors.
+#define LG_U 4
+
+template <class T>
 __global__ __launch_bounds__(256) void wr_logp_grad_kernel(LogpGradArgs a) {
-  for (int64_t row = blockIdx.x; row < a.f.n; row += gridDim.x) {
+  constexpr int VW = 16 / sizeof(T);
+  const int rt = a.row_threads, t0 = threadIdx.x % rt, v = a.f.v;
+  const int64_t items = a.f.n * a.splits, step = (int64_t)gridDim.x * (256 / rt);
+  for (int64_t item = (int64_t)blockIdx.x * (256 / rt) + threadIdx.x / rt; item < items; item += step) {
+    const int64_t row = a.splits > 1 ? item / a.splits : item;
+    const int seg = a.splits > 1 ? (int)(item % a.splits) : 0;
     const int64_t t = row_token(a.f, row);
     const T* z = (const T*)a.f.logits + row * a.f.stride;
     T* dz = (T*)a.dlogits + row * a.dstride;
     const float lse = t < 0 ? 0.0f : a.lse_in[row];
-    if (t < 0 || lse == -__builtin_inff()) {   // padding, or every class masked
-      for (int j = threadIdx.x; j < a.f.v; j += 256) dz[j] = (T)0.0f;
-      continue;
-    }
-    float gl = a.g_logp ? a.g_logp[row] : 0.0f, gp = (a.g_lse ? a.g_lse[row] : 0.0f) - gl;
-    const float gh = a.g_entropy ? a.g_entropy[row] : 0.0f, h = a.g_entropy ? a.entropy_in[row] : 0.0f;
-    if (a.g_logp && t >= a.f.v) gp = __builtin_nanf("");
-    for (int k = 0; k < a.f.top; ++k)
-      if (a.f.top_idx[row * a.f.top + k] >= 0) gp -= a.g_top[row * a.f.top + k];
-    for (int j = threadIdx.x; j < a.f.v; j += 256) {
-      const float lp = (float)z[j] - lse, p = fexp(lp);
-      float g = p * (gp - gh * (fmaxf(lp, WR_FAR) + h));
-      if (j == t) g += gl;
+    const bool zero = t < 0 || lse == -__builtin_inff();   // padding, or every class masked
+    const float gl = a.g_logp && !zero ? a.g_logp[row] : 0.0f;
+    const float gh = a.g_entropy && !zero ? a.g_entropy[row] : 0.0f, h = a.g_entropy && !zero ? a.entropy_in[row] : 0.0f;
+    float gp = (a.g_lse && !zero ? a.g_lse[row] : 0.0f) - gl;
+    if (a.g_logp && t >= v) gp = __builtin_nanf("");
+    const int32_t* ti = a.f.top_idx + row * a.f.top;
+    const float* tg = a.g_top + row * a.f.top;
+    if (!zero)
       for (int k = 0; k < a.f.top; ++k)
-        if (a.f.top_idx[row * a.f.top + k] == j) g += a.g_top[row * a.f.top + k];
-      dz[j] = (T)g;
+        if (ti[k] >= 0) gp -= tg[k];
+    float x[LG_U][VW];
+    const int64_t i0 = ((int64_t)seg * LG_U * rt + t0) * VW;
+#pragma unroll
+    for (int u = 0; u < LG_U; ++u) {
+      const int64_t j = i0 + (int64_t)u * rt * VW;
+      load_part<T, VW>(z + j, x[u], zero || j >= v ? 0 : (int)(v - j));
+    }
+#pragma unroll
+    for (int u = 0; u < LG_U; ++u) {
+      const int64_t j = i0 + (int64_t)u * rt * VW;
+      if (j >= v) break;
+      if (!zero) {
+#pragma unroll
+        for (int k = 0; k < VW; ++k) {
+          const float lp = x[u][k] - lse;
+          x[u][k] = fexp(lp) * (gp - gh * (fmaxf(lp, WR_FAR) + h));
+        }
+        if (t >= j && t < j + VW)
+#pragma unroll
+          for (int k = 0; k < VW; ++k)
+            if (t == j + k) x[u][k] += gl;
+        for (int i = 0; i < a.f.top; ++i)
+          if (ti[i] >= j && ti[i] < j + VW)
+#pragma unroll
+            for (int k = 0; k < VW; ++k)
+              if (ti[i] == j + k) x[u][k] += tg[i];
+      }
+      store_part<T, VW>(dz + j, x[u], (int)(v - j));
     }
   }
 }
@@ -173,7 +543,7 @@ __global__ __launch_bounds__(256) void wr_logp_grad_kernel(LogpGradArgs a) {
 wavernn_status check_logits(const char* name, int dtype, const void* p, int64_t n, int32_t v, int64_t stride, bool output) {
   if (!wr_dtype_ok(dtype)) return wr_fail(WAVERNN_E_INVALID, "bad dtype %d", dtype);
   if (n < 0 || n > INT32_MAX) return wr_fail(WAVERNN_E_INVALID, "n_rows %lld out of range", (long long)n);
-  if (v < 1) return wr_fail(WAVERNN_E_INVALID, "n_classes %d: must be positive", v);
+  if (v < 1 || v > (1 << 30)) return wr_fail(WAVERNN_E_INVALID, "n_classes %d not in [1, 2^30]", v);
   return wr_check_rows(name, p, dtype, n, v, stride, output);
 }
 wavernn_status check_tokens(const void* tokens, int bytes, int* kind) {
@@ -185,18 +555,41 @@ wavernn_status check_tokens(const void* tokens, int bytes, int* kind) {
 
 }  // namespace
 
+// Segments of a row: one, unless there are too few rows for the card (a row each for fewer than 512
+// blocks, two a CU) and they are long: then as many as give 1,024 blocks, of 4,096 classes at least.
+static int logp_splits(int64_t n, int32_t v) {
+  if (n < 1 || n >= 512) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({LW_SPLITS, 1024 / n, ((int64_t)v + 4095) / 4096}));
+}
+
+template <class T>
+static wavernn_status logp_launch(LogpArgs& a, void* stream) {
+  constexpr int VW = 16 / sizeof(T);
+  const int vecs = (int)(((int64_t)a.v + VW - 1) / VW);
+  auto blocks = [&](int rows) { return std::min<int64_t>((a.n + rows - 1) / rows, LOGP_BLOCKS); };
+  if (vecs <= 16) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 1>), blocks(16), 256, 0, stream, a);
+  else if (vecs <= 64) WR_LAUNCH((wr_logp_rows_kernel<T, 64, 1>), blocks(4), 256, 0, stream, a);
+  else if (vecs <= 256) WR_LAUNCH((wr_logp_rows_kernel<T, 64, 4>), blocks(4), 256, 0, stream, a);
+  else {
+    a.splits = a.part ? logp_splits(a.n, a.v) : 1;
+    a.seg = (int)(((int64_t)a.v + a.splits - 1) / a.splits + 7) / 8 * 8;
+    a.part_keys = (u64*)((LogpPart*)a.part + a.n * a.splits);
+    WR_LAUNCH((wr_logp_kernel<T>), std::min<int64_t>(a.n * a.splits, LOGP_BLOCKS), 256, 0, stream, a);
+    if (a.splits > 1) WR_LAUNCH((wr_logp_join_kernel<T>), a.n, 256, 0, stream, a);
+  }
+  return WAVERNN_OK;
+}
 wavernn_status wr_logp_launch(int dtype, LogpArgs& a, void* stream) {
   if (a.n == 0) return WAVERNN_OK;
-  const int64_t grid = std::min<int64_t>(a.n, WR_OP_BLOCKS);
-  WR_DISPATCH(dtype, T, WR_LAUNCH((wr_logp_kernel<T>), grid, 256, 0, stream, a));
-  return WAVERNN_OK;
+  WR_DISPATCH(dtype, T, return logp_launch<T>(a, stream));
 }
 
 extern "C" {
 
 int64_t wavernn_token_logprobs_workspace(int64_t n_rows, int32_t n_classes, int32_t top) {
-  if (n_rows < 0 || n_rows > INT32_MAX || n_classes < 1 || top < 0 || top > WAVERNN_MAX_TOP || top > n_classes) return -1;
-  return 0;
+  if (n_rows < 0 || n_rows > INT32_MAX || n_classes < 1 || n_classes > (1 << 30) || top < 0 || top > WAVERNN_MAX_TOP || top > n_classes) return -1;
+  const int s = logp_splits(n_rows, n_classes);
+  return s > 1 ? n_rows * s * (int64_t)(sizeof(LogpPart) + 8 * top) : 0;
 }
 
 wavernn_status wavernn_token_logprobs(int32_t dtype, const void* logits_dev, int64_t n_rows, int32_t n_classes,
@@ -225,6 +618,7 @@ wavernn_status wavernn_token_logprobs(int32_t dtype, const void* logits_dev, int
   a.lse = lse_dev;
   a.top_logp = top_logp_dev;
   a.top_idx = top_idx_dev;
+  a.part = need > 0 ? workspace_dev : nullptr;
   return wr_logp_launch(dtype, a, stream);
 }
 
@@ -263,7 +657,10 @@ wavernn_status wavernn_token_logprobs_grad(int32_t dtype, const void* logits_dev
   a.g_top = g_top_dev;
   a.dlogits = dlogits_dev;
   a.dstride = dlogits_stride;
-  const int64_t grid = std::min<int64_t>(n_rows, WR_OP_BLOCKS);
+  const int64_t vecs = ((int64_t)n_classes * wr_dtype_bytes(dtype) + 15) / 16;
+  a.row_threads = wr_row_threads((vecs + LG_U - 1) / LG_U);
+  a.splits = (int)((vecs + 256 * LG_U - 1) / (256 * LG_U));
+  const int64_t per = 256 / a.row_threads, grid = std::min<int64_t>((n_rows * a.splits + per - 1) / per, WR_OP_BLOCKS);
   WR_DISPATCH(dtype, T, WR_LAUNCH((wr_logp_grad_kernel<T>), grid, 256, 0, stream, a));
   return WAVERNN_OK;
 }

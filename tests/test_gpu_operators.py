@@ -164,12 +164,15 @@ def test_logprobs_special_rows(n, v, dt):
 
 
 @pytest.mark.parametrize("v", [256, 4096, 40000, 131072])
-@pytest.mark.parametrize("order", ["rising", "falling", "clustered", "same16", "few"])
+@pytest.mark.parametrize("order", ["rising", "falling", "clustered", "same16", "few", "apart", "three"])
 def test_logprobs_alternatives_in_any_place(v, order):
     """The alternatives may lie anywhere: side by side, at one distance, among many equal ones."""
     j = torch.arange(v, device="cuda", dtype=F32)
     z = {"rising": j / v, "falling": -j / v, "clustered": torch.where((j > v // 2) & (j < v // 2 + 70), 2.0 + j / v, 0.0),
-         "same16": (j % 16 == 3) * (1.0 + j / v), "few": torch.floor(j / (v / 5.0))}[order]
+         "same16": (j % 16 == 3) * (1.0 + j / v), "few": torch.floor(j / (v / 5.0)),
+         # a thousand large ones 1,024 or 2,048 classes apart and next to those; all but three masked
+         "apart": torch.where(j % 2048 < 64, 1.0 + j / v, 0.0),
+         "three": torch.where((j == 3) | (j == v // 2) | (j == v - 1), j / v, -INF)}[order]
     z = torch.stack([z, z.flip(0), z[torch.randperm(v, generator=gen(2), device="cuda")]])
     for dt in (F32, BF16):
         for top in (1, 7, 32):

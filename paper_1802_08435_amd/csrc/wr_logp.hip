@@ -85,16 +85,15 @@ __device__ __forceinline__ void soft_term(float z, float base, float& s, float& 
   s += e;
   w = __builtin_fmaf(fmaxf(d, WR_FAR), e, w);
 }
-__device__ __forceinline__ float soft_lse(Soft q) { return soft_base(q.m) + logf(q.s); }
-// What is taken from a logit for its log probability: nothing where every class is masked (q.s = 0).
-__device__ __forceinline__ float soft_sub(Soft q) { return q.s == 0.0f ? 0.0f : soft_lse(q); }
+// What is taken from a logit for its log probability: log sum exp, or nothing where every class is masked (q.s = 0).
+__device__ __forceinline__ float soft_sub(Soft q) { return q.s == 0.0f ? 0.0f : soft_base(q.m) + logf(q.s); }
 __device__ __forceinline__ float soft_entropy(Soft q) { return q.s == 0.0f ? 0.0f : logf(q.s) - q.w / q.s; }
 
 template <class T>
-__device__ __forceinline__ void put_row(const LogpArgs& a, int64_t o, int64_t t, const T* z, Soft q) {
-  if (a.logp) a.logp[o] = t < a.v ? (float)z[t] - soft_sub(q) : __builtin_nanf("");
+__device__ __forceinline__ void put_row(const LogpArgs& a, int64_t o, int64_t t, const T* z, Soft q, float sub) {
+  if (a.logp) a.logp[o] = t < a.v ? (float)z[t] - sub : __builtin_nanf("");
   if (a.entropy) a.entropy[o] = soft_entropy(q);
-  if (a.lse) a.lse[o] = soft_lse(q);
+  if (a.lse) a.lse[o] = q.s == 0.0f ? -__builtin_inff() : sub;
 }
 __device__ __forceinline__ void put_padding(const LogpArgs& a, int64_t o, int i) {
   if (i == 0) {
@@ -109,7 +108,7 @@ __device__ __forceinline__ void put_padding(const LogpArgs& a, int64_t o, int i)
 // Reductions over RT = 16 lanes by rotations within a row of 16 (every lane gets the result, in the same bits, as
 // each step only exchanges the operands of a commutative operation), over 64 by joining the four rows' results.
 template <int N>
-__device__ __forceinline__ int rotate16(int v) { return __builtin_amdgcn_update_dpp(v, v, 0x120 + N, 0xf, 0xf, false); }
+__device__ __forceinline__ int rotate16(int v) { return __builtin_amdgcn_update_dpp(0, v, 0x120 + N, 0xf, 0xf, true); }
 template <int RT, class F>
 __device__ __forceinline__ int group_reduce(int v, F f) {
   v = f(v, rotate16<8>(v));
@@ -142,11 +141,79 @@ __device__ __forceinline__ uint32_t group_umin(uint32_t v) {
   return (uint32_t)group_reduce<RT>((int)v, [](int a, int b) { return (int)((uint32_t)a < (uint32_t)b ? (uint32_t)a : (uint32_t)b); });
 }
 
+// One vector's classes c, c + 1, ... in the order of the alternatives; ones past the row's v
+// classes come last, with key 0.  pop() takes the first away.
+template <class T>
+struct TopVec {   // 16-bit logits: rank and number in one word, all different, sorted by a merge network (Batcher, 1968)
+  uint32_t key[8];
+  __device__ __forceinline__ void init(const float (&z)[8], int c, int v) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      uint32_t u;
+      if constexpr (__is_same(T, __bf16)) u = top_rank(z[k]) >> 16;   // a bf16's bits are a float's upper half
+      else {
+        const uint32_t h = __builtin_bit_cast(uint16_t, (_Float16)(z[k] + 0.0f));
+        u = z[k] != z[k] ? 0xffffu : (h >> 15) ? ~h & 0xffffu : h | 0x8000u;
+      }
+      key[k] = c + k < v ? u << 16 | (uint32_t)(0xffff - (c + k)) : 0;
+    }
+    constexpr int net[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
+                                {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
+#pragma unroll
+    for (int i = 0; i < 19; ++i) {
+      const uint32_t x = key[net[i][0]], y = key[net[i][1]];
+      key[net[i][0]] = x > y ? x : y;
+      key[net[i][1]] = x > y ? y : x;
+    }
+  }
+  __device__ __forceinline__ uint32_t at(int) const { return 0; }   // (in the key)
+  __device__ __forceinline__ void pop(bool on) {
+#pragma unroll
+    for (int k = 0; k < 7; ++k) key[k] = on ? key[k + 1] : key[k];
+    if (on) key[7] = 0;
+  }
+  static __device__ __forceinline__ int number(uint32_t key, uint32_t) { return 0xffff - (int)(key & 0xffffu); }
+  static __device__ __forceinline__ float value(uint32_t key) {
+    if constexpr (__is_same(T, __bf16)) return key_value((u64)(key & 0xffff0000u) << 32 | ((key >> 31) ? 0ull : 0xffffull << 32));
+    const uint32_t u = key >> 16;
+    return u == 0xffffu ? __builtin_nanf("")
+                        : (float)__builtin_bit_cast(_Float16, (uint16_t)((u >> 15) ? u & 0x7fffu : ~u));
+  }
+};
+template <>
+struct TopVec<float> {   // sorted by neighbours' exchanges, which keep equal logits in their order
+  uint32_t key[4], k_[4];
+  __device__ __forceinline__ void init(const float (&z)[4], int c, int v) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) key[k] = c + k < v ? top_rank(z[k]) : 0, k_[k] = k;
+    constexpr int net[6] = {0, 2, 1, 0, 2, 1};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) {
+      const int x = net[i], y = x + 1;
+      const bool swap = key[y] > key[x];
+      const uint32_t a = key[x], b = k_[x];
+      key[x] = swap ? key[y] : a, k_[x] = swap ? k_[y] : b;
+      key[y] = swap ? a : key[y], k_[y] = swap ? b : k_[y];
+    }
+  }
+  __device__ __forceinline__ uint32_t at(int c) const { return (uint32_t)c + k_[0]; }
+  __device__ __forceinline__ void pop(bool on) {
+#pragma unroll
+    for (int k = 0; k < 3; ++k) key[k] = on ? key[k + 1] : key[k], k_[k] = on ? k_[k + 1] : k_[k];
+    if (on) key[3] = 0;
+  }
+  static __device__ __forceinline__ int number(uint32_t, uint32_t at) { return (int)at; }
+  static __device__ __forceinline__ float value(uint32_t key) { return key_value((u64)key << 32); }
+};
+
 // Rows of up to RT * E vectors of 16 bytes, in registers: class (e RT + lane) VW + k.
-// The alternatives are drawn one by one: each lane offers its best class left.
+// Each vector is sorted for itself; then the alternatives are drawn one by one, each
+// lane offering its best class left.  With 16 lanes a row four rows share every
+// reduction of a wave.
 template <class T, int RT, int E>
 __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
   constexpr int VW = 16 / sizeof(T), KR = (WAVERNN_MAX_TOP + RT - 1) / RT;
+  constexpr bool packed = sizeof(T) == 2;
   const int lane = threadIdx.x % RT;
   const int64_t step = (int64_t)gridDim.x * (256 / RT);
   for (int64_t row = (int64_t)blockIdx.x * (256 / RT) + threadIdx.x / RT; row < a.n; row += step) {
@@ -173,42 +240,35 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
       for (int k = 0; k < VW; ++k) soft_term(z[e][k], base, q.s, q.w);
     q.s = group_fsum<RT>(q.s);
     q.w = group_fsum<RT>(q.w);
-    if (lane == 0) put_row(a, o, t, zr, q);
+    const float sub = soft_sub(q);
+    if (lane == 0) put_row(a, o, t, zr, q, sub);
     if (a.top == 0) continue;
-    uint32_t key[E][VW], best = 0, at = 0, won[KR] = {}, won_at[KR] = {};
+    TopVec<T> vec[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-#pragma unroll
-      for (int k = 0; k < VW; ++k) key[e][k] = (e * RT + lane) * VW + k < a.v ? top_rank(z[e][k]) : 0;
-    auto offer = [&]() {   // the lane's best class left, the lowest among equal ones
-      best = 0, at = 0xffffffffu;
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-#pragma unroll
-        for (int k = 0; k < VW; ++k)
-          if (key[e][k] > best) best = key[e][k], at = (e * RT + lane) * VW + k;
-    };
-    offer();
+    for (int e = 0; e < E; ++e) vec[e].init(z[e], (e * RT + lane) * VW, a.v);
+    uint32_t won[KR] = {}, won_at[KR] = {};
     for (int i = 0; i < a.top; ++i) {
-      const uint32_t m = group_umax<RT>(best), j = group_umin<RT>(best == m ? at : 0xffffffffu);
+      uint32_t best = vec[0].key[0], at = vec[0].at(lane * VW);
+#pragma unroll
+      for (int e = 1; e < E; ++e) {
+        const bool more = vec[e].key[0] > best;
+        best = more ? vec[e].key[0] : best;
+        if constexpr (!packed) at = more ? vec[e].at((e * RT + lane) * VW) : at;
+      }
+      const uint32_t m = group_umax<RT>(best);
+      uint32_t j = 0;
+      if constexpr (!packed) j = group_umin<RT>(best == m ? at : 0xffffffffu);
 #pragma unroll
       for (int r = 0; r < KR; ++r)
         if (lane + r * RT == i) won[r] = m, won_at[r] = j;
-      if (at == j) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-#pragma unroll
-          for (int k = 0; k < VW; ++k)
-            if ((uint32_t)((e * RT + lane) * VW + k) == j) key[e][k] = 0;
-        offer();
-      }
+      for (int e = 0; e < E; ++e) vec[e].pop(packed ? vec[e].key[0] == m : vec[e].at((e * RT + lane) * VW) == j);
     }
-    const float sub = soft_sub(q);
 #pragma unroll
     for (int r = 0; r < KR; ++r)
       if (lane + r * RT < a.top) {
-        a.top_idx[o * a.top + lane + r * RT] = (int)won_at[r];
-        a.top_logp[o * a.top + lane + r * RT] = key_value((u64)won[r] << 32) - sub;
+        a.top_idx[o * a.top + lane + r * RT] = TopVec<T>::number(won[r], won_at[r]);
+        a.top_logp[o * a.top + lane + r * RT] = TopVec<T>::value(won[r]) - sub;
       }
   }
 }
@@ -422,7 +482,7 @@ __global__ __launch_bounds__(256) void wr_logp_kernel(LogpArgs a) {
     __syncthreads();
     q = soft_join(soft_join(sh.soft[0], sh.soft[1]), soft_join(sh.soft[2], sh.soft[3]));
     if (tid == 0) {
-      if (a.splits == 1) put_row(a, o, t, zr, q);
+      if (a.splits == 1) put_row(a, o, t, zr, q, soft_sub(q));
       else ((LogpPart*)a.part)[item].q = q;
     }
     if (a.top > 0) {
@@ -450,7 +510,7 @@ __global__ __launch_bounds__(256) void wr_logp_join_kernel(LogpArgs a) {
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1)
       q = soft_join(q, Soft{__shfl_xor(q.m, d, 64), __shfl_xor(q.s, d, 64), __shfl_xor(q.w, d, 64)});
-    if (tid == 0) put_row(a, o, t, (const T*)a.logits + row * a.stride, q);
+    if (tid == 0) put_row(a, o, t, (const T*)a.logits + row * a.stride, q, soft_sub(q));
     if (a.top == 0) continue;
     // The segments' best classes come first: the top-th largest of them is a lower bound, reached in at
     // most `top` segments, so at most top^2 classes are ranked.
@@ -568,7 +628,7 @@ static wavernn_status logp_launch(LogpArgs& a, void* stream) {
   const int vecs = (int)(((int64_t)a.v + VW - 1) / VW);
   auto blocks = [&](int rows) { return std::min<int64_t>((a.n + rows - 1) / rows, LOGP_BLOCKS); };
   if (vecs <= 16) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 1>), blocks(16), 256, 0, stream, a);
-  else if (vecs <= 64) WR_LAUNCH((wr_logp_rows_kernel<T, 64, 1>), blocks(4), 256, 0, stream, a);
+  else if (vecs <= 64) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 4>), blocks(16), 256, 0, stream, a);
   else if (vecs <= 256) WR_LAUNCH((wr_logp_rows_kernel<T, 64, 4>), blocks(4), 256, 0, stream, a);
   else {
     a.splits = a.part ? logp_splits(a.n, a.v) : 1;

@@ -179,6 +179,18 @@ def test_logprobs_alternatives_in_any_place(v, order):
             check_logp(z.to(dt), tokens_for(3, v), top)
 
 
+@pytest.mark.parametrize("order", ["apart", "few", "three", "equal"])
+def test_logprobs_alternatives_of_many_long_rows(order):
+    """Enough rows that none is taken in segments, and more classes tie or lie close than are ranked at once."""
+    n, v = 520, 40000
+    j = torch.arange(v, device="cuda", dtype=F32)
+    z = {"apart": torch.where(j % 2048 < 64, 1.0 + j / v, 0.0), "few": torch.floor(j / (v / 5.0)),
+         "three": torch.where((j == 3) | (j == v // 2) | (j == v - 1), j / v, -INF), "equal": torch.zeros_like(j)}[order]
+    z = torch.stack([torch.roll(z, 64 * i) for i in range(n)])
+    for dt, top in ((F32, 9), (BF16, 9), (F16, 32)):
+        check_logp(z.to(dt), tokens_for(n, v), top)
+
+
 @MIX
 def test_logprobs_views_and_token_types(dt):
     base = randn(6, 10, 300, seed=4, dt=dt, scale=2.0)

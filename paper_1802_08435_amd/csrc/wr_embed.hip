@@ -66,11 +66,14 @@ __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
 // passes in LDS; more take two launches a pass (digit counts of every tile, then the
 // scatter), tiles of SORT_TILE ids, at most 256 tiles.
 //
-// Sum: chunks of EG_CHUNK sorted positions, one group of threads a chunk, each
-// thread one vector of columns, EG_AHEAD rows in flight.  A run inside a chunk is
-// written to the table; the parts of a run that crosses chunks go to the
-// workspace (slot 0: the chunk's beginning, slot 1: its end), and the third launch
-// adds them in chunk order.  Blocks behind the chunks' clear the rows of absent numbers.
+// The sort leaves the memory idle, so further blocks of its launches clear the table
+// meanwhile, all of it: which rows stay without a number is not known yet.
+//
+// Sum: chunks of sorted positions, one group of threads a chunk, each thread one
+// vector of columns, EG_AHEAD rows in flight.  A run inside a chunk is written to
+// the table; the parts of a run that crosses chunks go to the workspace
+// (slot 0: the chunk's beginning, slot 1: its end), and one more launch adds them
+// in chunk order.
 #define SORT_THREADS 1024
 #define SORT_WAVES 16
 #define SORT_BITS 9
@@ -78,8 +81,10 @@ __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
 #define SORT_SMALL 4096
 #define SORT_TILE 2048
 #define SORT_TILES 256
-#define EG_CHUNK 32
 #define EG_AHEAD 8
+#define EG_CHUNK_MIN 8      // positions of a chunk: doubled up to 64 while that leaves 1,024 blocks, four a CU (and 64 KiB of LDS are enough)
+#define EG_CHUNK_MAX 64
+#define EG_CLEAR 65536      // bytes that a block clears
 
 struct EmbedGradArgs {
   const void* dout;
@@ -97,8 +102,10 @@ struct EmbedGradArgs {
   int src, shift;               // of one pass: buffer read (-1: the ids), digit's lowest bit
   const uint32_t *skey, *spos;  // sorted
   float* part;                  // [chunks][2][dim]
-  int chunks, row_threads;      // row_threads: threads on a row (256 / row_threads chunks a block)
-  int chunk_blocks, clear_rows; // blocks of the sum on chunks; rows that each block behind them clears
+  int chunk, chunks;            // positions of a chunk
+  int row_threads;              // threads on a row (256 / row_threads chunks a block)
+  int sort_blocks;              // of a sort's launch; the ones behind them clear bytes clear0 .. clear1 of dtable
+  int64_t clear0, clear1;
 };
 
 __device__ __forceinline__ uint32_t sort_key(const EmbedGradArgs& a, int i) {
@@ -158,6 +165,23 @@ __device__ __forceinline__ void scan_bins(uint32_t* x, uint32_t* tmp) {
   __syncthreads();
 }
 
+// Clears this block's part of the table (any alignment; whole 16-byte pieces and the ends by element).
+__device__ void clear_part(const EmbedGradArgs& a) {
+  const int64_t step = (int64_t)(gridDim.x - a.sort_blocks) * EG_CLEAR;
+  for (int64_t b0 = a.clear0 + (int64_t)(blockIdx.x - a.sort_blocks) * EG_CLEAR; b0 < a.clear1; b0 += step) {
+    unsigned char* p = (unsigned char*)a.dtable + b0;
+    const int n = (int)std::min<int64_t>(EG_CLEAR, a.clear1 - b0);
+    for (int i = threadIdx.x * 16; i < n; i += SORT_THREADS * 16) {
+      if (i + 16 <= n) {
+        const uint4 z = {0, 0, 0, 0};
+        __builtin_memcpy(p + i, &z, 16);
+      } else {
+        for (int j = i; j < n; j += 2) *(uint16_t*)(p + j) = 0;
+      }
+    }
+  }
+}
+
 // All passes by one block, n <= SORT_SMALL.
 __global__ __launch_bounds__(SORT_THREADS) void wr_sort_small_kernel(EmbedGradArgs a) {
   constexpr int E = SORT_SMALL / SORT_THREADS;
@@ -165,6 +189,7 @@ __global__ __launch_bounds__(SORT_THREADS) void wr_sort_small_kernel(EmbedGradAr
   __shared__ uint32_t keys[SORT_SMALL];
   __shared__ uint16_t poss[SORT_SMALL];
   __shared__ uint32_t base[SORT_BINS], tmp[16];
+  if ((int)blockIdx.x >= a.sort_blocks) return clear_part(a);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   uint32_t k[E];
   int p[E], r[E];
@@ -210,6 +235,7 @@ __global__ __launch_bounds__(SORT_THREADS) void wr_sort_small_kernel(EmbedGradAr
 // Counts of the pass's digits in each tile.
 __global__ __launch_bounds__(SORT_THREADS) void wr_sort_count_kernel(EmbedGradArgs a) {
   __shared__ uint32_t h[SORT_BINS];
+  if ((int)blockIdx.x >= a.sort_blocks) return clear_part(a);
   const uint32_t mask = (1u << a.bits) - 1;
   if (threadIdx.x < SORT_BINS) h[threadIdx.x] = 0;
   __syncthreads();
@@ -226,6 +252,7 @@ __global__ __launch_bounds__(SORT_THREADS) void wr_sort_scatter_kernel(EmbedGrad
   constexpr int E = SORT_TILE / SORT_THREADS;
   __shared__ uint16_t cnt[SORT_WAVES][SORT_BINS];
   __shared__ uint32_t base[SORT_BINS], before[2][SORT_BINS], total[2][SORT_BINS], tmp[16];
+  if ((int)blockIdx.x >= a.sort_blocks) return clear_part(a);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const uint32_t mask = (1u << a.bits) - 1;
   {   // this tile's first place of each digit: all smaller digits, and this one in the tiles before
@@ -280,134 +307,106 @@ __global__ __launch_bounds__(SORT_THREADS) void wr_sort_scatter_kernel(EmbedGrad
   }
 }
 
-// Chunk c's columns of thread t of its row threads.
-template <class T, class U>
-__device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, int64_t c, int t) {
-  constexpr int VW = vec_of<T, U>();
-  const int rt = a.row_threads;
-  U* table = (U*)a.dtable;
-  const int64_t p0 = c * EG_CHUNK, p1 = std::min<int64_t>(a.n, p0 + EG_CHUNK);
-  const uint32_t first = a.skey[p0], last = a.skey[p1 - 1];
-  const bool from = p0 > 0 && a.skey[p0 - 1] == first, on = p1 < a.n && a.skey[p1] == last;
-  for (int col = t * VW; col < a.dim; col += rt * VW) {
-    const int count = a.dim - col;
-    float acc[VW];
-    uint32_t cur = first;
-    auto flush = [&](uint32_t id, bool at_end) {
-      if (id >= (uint32_t)a.v) return;
-      if (id == first && from) store_part<float, VW>(a.part + (2 * c) * a.dim + col, acc, count);
-      else if (at_end && on) store_part<float, VW>(a.part + (2 * c + 1) * a.dim + col, acc, count);
-      else {
-#pragma unroll
-        for (int i = 0; i < VW; ++i) acc[i] *= a.scale;
-        store_part<U, VW>(table + (int64_t)id * a.dim + col, acc, count);
-      }
-    };
-#pragma unroll
-    for (int i = 0; i < VW; ++i) acc[i] = 0.0f;
-    for (int64_t p = p0; p < p1; p += EG_AHEAD) {
-      uint32_t id[EG_AHEAD];
-      float x[EG_AHEAD][VW];
-#pragma unroll
-      for (int u = 0; u < EG_AHEAD; ++u) {
-        id[u] = p + u < p1 ? a.skey[p + u] : (uint32_t)a.v;
-        if (id[u] < (uint32_t)a.v)
-          load_part<T, VW>((const T*)a.dout + (int64_t)a.spos[p + u] * a.dout_stride + col, x[u], count);
-      }
-#pragma unroll
-      for (int u = 0; u < EG_AHEAD; ++u) {
-        if (p + u >= p1) break;
-        if (id[u] != cur) {
-          flush(cur, false);
-          cur = id[u];
-#pragma unroll
-          for (int i = 0; i < VW; ++i) acc[i] = 0.0f;
-        }
-        if (id[u] < (uint32_t)a.v)
-#pragma unroll
-          for (int i = 0; i < VW; ++i) acc[i] += x[u][i];
-      }
-    }
-    flush(cur, true);
-  }
-}
-
+// LDS: the numbers and positions of the block's chunks.
 template <class T, class U>
 __global__ __launch_bounds__(256) void wr_embed_sum_kernel(EmbedGradArgs a) {
+  extern __shared__ uint32_t at[];
   constexpr int VW = vec_of<T, U>();
-  const int rt = a.row_threads, g = threadIdx.x / rt, t = threadIdx.x % rt;
+  const int rt = a.row_threads, t = threadIdx.x % rt, per = 256 / rt * a.chunk;
   U* table = (U*)a.dtable;
-  if ((int)blockIdx.x < a.chunk_blocks) {
-    for (int64_t c = (int64_t)blockIdx.x * (256 / rt) + g; c < a.chunks; c += (int64_t)a.chunk_blocks * (256 / rt))
-      sum_chunk<T, U>(a, c, t);
-    return;
-  }
-  // rows without a number
-  __shared__ int absent[256];
-  for (int64_t v0 = (int64_t)(blockIdx.x - a.chunk_blocks) * a.clear_rows; v0 < a.v;
-       v0 += (int64_t)(gridDim.x - a.chunk_blocks) * a.clear_rows) {
-    const int nr = (int)std::min<int64_t>(a.clear_rows, a.v - v0);
-    if ((int)threadIdx.x < nr) {
-      const uint32_t v = (uint32_t)(v0 + threadIdx.x);
-      int lo = 0, hi = a.n;
-      while (lo < hi) {
-        const int mid = (int)(((int64_t)lo + hi) / 2);
-        if (a.skey[mid] < v) lo = mid + 1;
-        else hi = mid;
-      }
-      absent[threadIdx.x] = lo >= a.n || a.skey[lo] != v;
-    }
+  for (int64_t b0 = (int64_t)blockIdx.x * per; b0 < a.n; b0 += (int64_t)gridDim.x * per) {
     __syncthreads();
-    float zero[VW];
+    for (int i = threadIdx.x; i < per && b0 + i < a.n; i += 256) at[i] = a.skey[b0 + i], at[per + i] = a.spos[b0 + i];
+    __syncthreads();
+    const int l0 = threadIdx.x / rt * a.chunk;            // this group's chunk, in LDS
+    const int64_t p0 = b0 + l0;
+    if (p0 >= a.n) continue;
+    const int m = (int)std::min<int64_t>(a.chunk, a.n - p0);
+    const int64_t c = p0 / a.chunk;
+    const uint32_t *key = at + l0, *pos = at + per + l0;
+    const uint32_t first = key[0], last = key[m - 1], v = (uint32_t)a.v;
+    const bool from = p0 > 0 && a.skey[p0 - 1] == first, on = p0 + m < a.n && a.skey[p0 + m] == last;
+    for (int col = t * VW; col < a.dim; col += rt * VW) {
+      const int count = a.dim - col;
+      float acc[VW];
+      uint32_t cur = first;
+      auto flush = [&](uint32_t id, bool at_end) {
+        if (id >= v) return;
+        if (id == first && from) store_part<float, VW>(a.part + (2 * c) * a.dim + col, acc, count);
+        else if (at_end && on) store_part<float, VW>(a.part + (2 * c + 1) * a.dim + col, acc, count);
+        else {
 #pragma unroll
-    for (int i = 0; i < VW; ++i) zero[i] = 0.0f;
-    for (int r = g; r < nr; r += 256 / rt)
-      if (absent[r])
-        for (int col = t * VW; col < a.dim; col += rt * VW) store_part<U, VW>(table + (v0 + r) * a.dim + col, zero, a.dim - col);
-    __syncthreads();
+          for (int i = 0; i < VW; ++i) acc[i] *= a.scale;
+          store_part<U, VW>(table + (int64_t)id * a.dim + col, acc, count);
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < VW; ++i) acc[i] = 0.0f;
+      for (int p = 0; p < m; p += EG_AHEAD) {
+        float x[EG_AHEAD][VW];
+#pragma unroll
+        for (int u = 0; u < EG_AHEAD; ++u)
+          if (p + u < m && key[p + u] < v)
+            load_part<T, VW>((const T*)a.dout + (int64_t)pos[p + u] * a.dout_stride + col, x[u], count);
+#pragma unroll
+        for (int u = 0; u < EG_AHEAD; ++u) {
+          if (p + u >= m) break;
+          const uint32_t id = key[p + u];
+          if (id != cur) {
+            flush(cur, false);
+            cur = id;
+#pragma unroll
+            for (int i = 0; i < VW; ++i) acc[i] = 0.0f;
+          }
+          if (id < v)
+#pragma unroll
+            for (int i = 0; i < VW; ++i) acc[i] += x[u][i];
+        }
+      }
+      flush(cur, true);
+    }
   }
 }
 
-// Runs that cross chunks: block c adds the parts of the run that begins in chunk c and goes on, in chunk order (each
-// group of threads every (256 / row_threads)-th part, then the groups in order).
+// Runs that cross chunks: block (c, s) adds, for up to 256 columns, the parts of the run that begins in chunk c and
+// goes on, in chunk order (each group of threads every groups-th part, then the groups in order).
 template <class U>
 __global__ __launch_bounds__(256) void wr_embed_join_kernel(EmbedGradArgs a) {
   __shared__ float sums[256][4];
+  const int rt = a.row_threads, groups = 256 / rt, g = threadIdx.x / rt, t = threadIdx.x % rt;
   for (int64_t c = blockIdx.x; c + 1 < a.chunks; c += gridDim.x) {
-    const int64_t p0 = c * EG_CHUNK, p1 = p0 + EG_CHUNK;
-    const uint32_t id = a.skey[p1 - 1];
-    if (id >= (uint32_t)a.v || a.skey[p1] != id || (a.skey[p0] == id && p0 > 0 && a.skey[p0 - 1] == id)) continue;
+    const int64_t p0 = c * a.chunk, p1 = p0 + a.chunk;
+    const uint32_t id = a.skey[p1 - 1], next = a.skey[p1], head = a.skey[p0], prev = p0 > 0 ? a.skey[p0 - 1] : ~0u;
+    if (id >= (uint32_t)a.v || next != id || (head == id && prev == id)) continue;
     int64_t more = 0;   // chunks after c that begin with the number
     for (;;) {
-      const int64_t p = (c + 1 + more + threadIdx.x) * EG_CHUNK;
+      const int64_t p = (c + 1 + more + threadIdx.x) * a.chunk;
       const int k = __syncthreads_count(p < a.n && a.skey[p] == id);
       more += k;
       if (k < 256) break;
     }
-    const int rt = a.row_threads, groups = 256 / rt, g = threadIdx.x / rt, t = threadIdx.x % rt;
-    for (int c0 = 0; c0 < a.dim; c0 += rt * 4) {
-      const int col = c0 + t * 4, count = a.dim - col;
-      float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (count > 0)
+    const int64_t col = ((int64_t)blockIdx.y * rt + t) * 4;
+    const int count = (int)std::min<int64_t>(4, a.dim - col);
+    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (count > 0)
 #pragma unroll 8
-        for (int64_t j = g; j <= more; j += groups) {
-          float x[4];
-          load_part<float, 4>(a.part + (2 * (c + j) + (j == 0)) * a.dim + col, x, count, 0.0f);
+      for (int64_t j = g; j <= more; j += groups) {
+        float x[4];
+        load_part<float, 4>(a.part + (2 * (c + j) + (j == 0)) * a.dim + col, x, count);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[i] += x[i];
-        }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sums[threadIdx.x][i] = acc[i];
-      __syncthreads();
-      if (g == 0 && count > 0) {
-        for (int k = 1; k < groups; ++k)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[i] += sums[k * rt + t][i];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] *= a.scale;
-        store_part<U, 4>((U*)a.dtable + (int64_t)id * a.dim + col, acc, count);
+        for (int i = 0; i < 4; ++i) acc[i] += x[i];
       }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[threadIdx.x][i] = acc[i];
+    __syncthreads();
+    if (g == 0 && count > 0) {
+      for (int k = 1; k < groups; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] += sums[k * rt + t][i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] *= a.scale;
+      store_part<U, 4>((U*)a.dtable + (int64_t)id * a.dim + col, acc, count);
     }
   }
 }
@@ -421,7 +420,11 @@ int64_t plan_embed_grad(int64_t n, int32_t dim, int64_t v, EmbedGradArgs* a, uns
   a->tile = SORT_TILE;
   while ((n + a->tile - 1) / a->tile > SORT_TILES) a->tile += SORT_TILE;
   a->tiles = (int)((n + a->tile - 1) / a->tile);
-  a->chunks = (int)((n + EG_CHUNK - 1) / EG_CHUNK);
+  // (by vectors of 4 elements, whatever the types, so that the workspace is known from the sizes)
+  const int64_t rt = wr_row_threads(((int64_t)dim + 3) / 4);
+  a->chunk = EG_CHUNK_MIN;
+  while (a->chunk < EG_CHUNK_MAX && n * rt / 256 / (2 * a->chunk) >= 1024 && 2 * a->chunk * 512 <= 8192 * rt) a->chunk *= 2;
+  a->chunks = (int)((n + a->chunk - 1) / a->chunk);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     unsigned char* p = ws + at;
@@ -441,29 +444,42 @@ int64_t plan_embed_grad(int64_t n, int32_t dim, int64_t v, EmbedGradArgs* a, uns
 template <class T, class U>
 wavernn_status run_embed_grad(EmbedGradArgs& a, void* stream) {
   int last = 0;
-  if (a.n > 0 && a.n <= SORT_SMALL) {
-    WR_LAUNCH(wr_sort_small_kernel, 1, SORT_THREADS, 0, stream, a);
-  } else if (a.n > 0) {
+  const bool small = a.n <= SORT_SMALL;
+  const int launches = small ? 1 : 2 * a.passes;
+  const int64_t bytes = (int64_t)a.v * a.dim * sizeof(U);
+  auto clear = [&](int i) {   // launch i's share of the table, in 16-byte pieces; its blocks
+    a.clear0 = bytes / 16 * i / launches * 16;
+    a.clear1 = i + 1 == launches ? bytes : bytes / 16 * (i + 1) / launches * 16;
+    return a.sort_blocks + std::min<int64_t>((a.clear1 - a.clear0 + EG_CLEAR - 1) / EG_CLEAR, 1 << 16);
+  };
+  if (small) {
+    a.sort_blocks = 1;
+    WR_LAUNCH(wr_sort_small_kernel, clear(0), SORT_THREADS, 0, stream, a);
+  } else {
+    a.sort_blocks = a.tiles;
     for (int pass = 0; pass < a.passes; ++pass) {
       a.src = pass == 0 ? -1 : (pass - 1) & 1;
       a.shift = pass * a.bits;
-      WR_LAUNCH(wr_sort_count_kernel, a.tiles, SORT_THREADS, 0, stream, a);
-      WR_LAUNCH(wr_sort_scatter_kernel, a.tiles, SORT_THREADS, 0, stream, a);
+      WR_LAUNCH(wr_sort_count_kernel, clear(2 * pass), SORT_THREADS, 0, stream, a);
+      WR_LAUNCH(wr_sort_scatter_kernel, clear(2 * pass + 1), SORT_THREADS, 0, stream, a);
     }
     last = (a.passes - 1) & 1;
   }
+  if (a.n == 0) return WAVERNN_OK;
   a.skey = a.key[last];
   a.spos = a.pos[last];
   constexpr int VW = vec_of<T, U>();
-  a.row_threads = wr_row_threads((a.dim + VW - 1) / VW);
-  a.chunk_blocks = (int)std::min<int64_t>(((int64_t)a.chunks * a.row_threads + 255) / 256, 1 << 20);
-  // a block clears about 128 KiB
-  a.clear_rows = (int)std::min<int64_t>(256, std::max<int64_t>(1, 131072 / ((int64_t)a.dim * sizeof(U))));
-  const int64_t clear_blocks = std::min<int64_t>(((int64_t)a.v + a.clear_rows - 1) / a.clear_rows, 1 << 20);
-  WR_LAUNCH((wr_embed_sum_kernel<T, U>), a.chunk_blocks + clear_blocks, 256, 0, stream, a);
+  a.row_threads = wr_row_threads(((int64_t)a.dim + VW - 1) / VW);
+  const int per = 256 / a.row_threads * a.chunk;
+  WR_LAUNCH((wr_embed_sum_kernel<T, U>), std::min<int64_t>(((int64_t)a.n + per - 1) / per, 1 << 20), 256, 8 * per, stream, a);
   if (a.chunks > 1) {
-    a.row_threads = wr_row_threads((a.dim + 3) / 4);
-    WR_LAUNCH((wr_embed_join_kernel<U>), std::min(a.chunks - 1, 1 << 20), 256, 0, stream, a);
+    a.row_threads = std::min(64, wr_row_threads(((int64_t)a.dim + 3) / 4));
+    void* argv[] = {&a};
+    const unsigned slices = (unsigned)(((int64_t)a.dim + 4 * a.row_threads - 1) / (4 * a.row_threads));
+    const unsigned blocks = (unsigned)std::min<int64_t>(a.chunks - 1, 1 << 16);
+    const hipError_t e = hipLaunchKernel((const void*)wr_embed_join_kernel<U>, dim3(blocks, slices), dim3(256), argv, 0,
+                                         (hipStream_t)stream);
+    if (e != hipSuccess) return wr_fail(WAVERNN_E_HIP, "launch of wr_embed_join_kernel: %s", hipGetErrorString(e));
   }
   return WAVERNN_OK;
 }
@@ -480,7 +496,7 @@ wavernn_status check_embed(int in_dtype, int out_dtype, int64_t n_table, int32_t
   if (out_dtype != in_dtype && out_dtype != WAVERNN_F32)
     return wr_fail(WAVERNN_E_INVALID, "the result's dtype must be the input's or F32");
   if (n_table < 1 || n_table > INT32_MAX) return wr_fail(WAVERNN_E_INVALID, "n_table %lld out of range", (long long)n_table);
-  if (dim < 1 || dim > (1 << 30)) return wr_fail(WAVERNN_E_INVALID, "dim %d not in [1, 2^30]", dim);
+  if (dim < 1 || dim > (1 << 20)) return wr_fail(WAVERNN_E_INVALID, "dim %d not in [1, 2^20]", dim);
   return WAVERNN_OK;
 }
 
@@ -507,7 +523,7 @@ wavernn_status wavernn_embed(int32_t table_dtype, const void* table_dev, int64_t
 }
 
 int64_t wavernn_embed_grad_workspace(int64_t n_ids, int32_t dim, int64_t n_table) {
-  if (n_ids < 0 || n_ids > INT32_MAX || dim < 1 || dim > (1 << 30) || n_table < 1 || n_table > INT32_MAX) return -1;
+  if (n_ids < 0 || n_ids > INT32_MAX || dim < 1 || dim > (1 << 20) || n_table < 1 || n_table > INT32_MAX) return -1;
   EmbedGradArgs a = {};
   return plan_embed_grad(n_ids, dim, n_table, &a, nullptr);
 }

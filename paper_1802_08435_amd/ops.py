@@ -17,6 +17,7 @@ import torch
 from . import wavernn as _w
 
 MAX_TOP = 32
+_raw_stream = torch._C._cuda_getCurrentRawStream    # (torch.cuda.current_stream() makes an object: 2.6 us)
 _DTYPE = {torch.float32: _w.F32, torch.bfloat16: _w.BF16, torch.float16: _w.F16}
 _ID_BYTES = {torch.int32: 4, torch.int64: 8}
 
@@ -64,17 +65,22 @@ def _plain(name, t, shape, dtypes, device):
     return t
 
 
-def _result(name, out, shape, dtype, device):
+def _result(name, out, shape, dtype, like):
     """A new tensor, or ``out`` checked to fit; with the distance between its rows."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device), shape[-1]
+        return like.new_empty(shape, dtype=dtype), shape[-1]
+    device = like.device
     if out.shape != shape or out.dtype != dtype or out.device != device:
         raise ValueError(f"{name}: needs {dtype} {list(shape)} on {device}, got {out.dtype} {list(out.shape)} on {out.device}")
     return out, _rows(name, out)[2]
 
 
-def _workspace(n_bytes, device):
-    return torch.empty(n_bytes, dtype=torch.uint8, device=device) if n_bytes > 0 else None
+def _workspace(n_bytes, like):
+    return like.new_empty(n_bytes, dtype=torch.uint8) if n_bytes > 0 else None
+
+
+def _p(t):
+    return None if t is None else t.data_ptr()
 
 
 def _on_gpu(fn):
@@ -82,7 +88,7 @@ def _on_gpu(fn):
     def call(t, *args, stream=None, **kw):
         if not t.is_cuda:
             raise ValueError(f"{fn.__name__}: tensors must be on a GPU")
-        if stream is None and t.device.index == torch.cuda.current_device():
+        if stream is None and t.device.index == torch._C._cuda_getDevice():
             return fn(t, *args, **kw)
         if stream is not None and stream.device != t.device:
             raise ValueError(f"{fn.__name__}: the stream is on {stream.device}, the tensors on {t.device}")
@@ -110,16 +116,20 @@ def token_logprobs(logits, tokens=None, top=0):
     if tokens is not None:
         _plain("tokens", tokens, shape, _IDS, dev)
     ws_bytes = L.wavernn_token_logprobs_workspace(n, v, top)
-    ws = _workspace(ws_bytes, dev)
-    new = lambda *s, dtype=torch.float32: torch.empty(*s, dtype=dtype, device=dev)
-    entropy, lse = new(shape), new(shape)
-    logp = new(shape) if tokens is not None else None
-    k = max(int(top), 0)
-    top_logp, top_idx = (new(*shape, k), new(*shape, k, dtype=torch.int32)) if k else (None, None)
-    _w._check(L.wavernn_token_logprobs(dt, _w._ptr(logits), n, v, stride, _w._ptr(tokens),
-                                       _ID_BYTES[tokens.dtype] if tokens is not None else 0, top, _w._ptr(logp),
-                                       _w._ptr(entropy), _w._ptr(lse), _w._ptr(top_logp), _w._ptr(top_idx), _w._ptr(ws),
-                                       max(ws_bytes, 0), _w._stream()))
+    ws = _workspace(ws_bytes, logits)
+    logp = None
+    if tokens is not None:                 # one allocation for the three
+        logp, entropy, lse = logits.new_empty((3, *shape), dtype=torch.float32).unbind()
+    else:
+        entropy, lse = logits.new_empty((2, *shape), dtype=torch.float32).unbind()
+    top_logp = top_idx = None
+    if top > 0:
+        top_logp = logits.new_empty((*shape, top), dtype=torch.float32)
+        top_idx = logits.new_empty((*shape, top), dtype=torch.int32)
+    _w._check(L.wavernn_token_logprobs(dt, _p(logits), n, v, stride, _p(tokens),
+                                       _ID_BYTES[tokens.dtype] if tokens is not None else 0, top, _p(logp),
+                                       _p(entropy), _p(lse), _p(top_logp), _p(top_idx), _p(ws),
+                                       max(ws_bytes, 0), _raw_stream(dev.index)))
     return dict(logp=logp, entropy=entropy, lse=lse, top_logp=top_logp, top_idx=top_idx)
 
 
@@ -144,12 +154,12 @@ def token_logprobs_grad(logits, tokens, lse, entropy=None, g_logp=None, g_entrop
         if top_idx is None:
             raise ValueError("g_top needs top_idx")
         _plain("top_idx", top_idx, shape + (k,), _I32, dev)
-    out, out_stride = _result("out", out, logits.shape, logits.dtype, dev)
-    _w._check(L.wavernn_token_logprobs_grad(dt, _w._ptr(logits), n, v, stride, _w._ptr(tokens),
-                                            _ID_BYTES[tokens.dtype] if tokens is not None else 0, _w._ptr(lse),
-                                            _w._ptr(entropy), _w._ptr(g_logp), _w._ptr(g_entropy), _w._ptr(g_lse), k,
-                                            _w._ptr(top_idx) if k else None, _w._ptr(g_top), _w._ptr(out), out_stride,
-                                            _w._stream()))
+    out, out_stride = _result("out", out, logits.shape, logits.dtype, logits)
+    _w._check(L.wavernn_token_logprobs_grad(dt, _p(logits), n, v, stride, _p(tokens),
+                                            _ID_BYTES[tokens.dtype] if tokens is not None else 0, _p(lse),
+                                            _p(entropy), _p(g_logp), _p(g_entropy), _p(g_lse), k,
+                                            _p(top_idx) if k else None, _p(g_top), _p(out), out_stride,
+                                            _raw_stream(dev.index)))
     return out
 
 
@@ -172,9 +182,9 @@ def embed(table, ids, scale=1.0, dtype=None, out=None):
     v, d, stride = _rows("table", table)
     _plain("ids", ids, ids.shape, _IDS, dev)
     dtype = _table_dtype("embed", dtype, table.dtype)
-    out, out_stride = _result("out", out, ids.shape + (d,), dtype, dev)
-    _w._check(L.wavernn_embed(dt, _w._ptr(table), v, d, stride, _w._ptr(ids), _ID_BYTES[ids.dtype], ids.numel(), scale,
-                              _DTYPE[dtype], _w._ptr(out), out_stride, _w._stream()))
+    out, out_stride = _result("out", out, ids.shape + (d,), dtype, table)
+    _w._check(L.wavernn_embed(dt, _p(table), v, d, stride, _p(ids), _ID_BYTES[ids.dtype], ids.numel(), scale,
+                              _DTYPE[dtype], _p(out), out_stride, _raw_stream(dev.index)))
     return out
 
 
@@ -188,10 +198,10 @@ def embed_grad(dout, ids, n_rows, scale=1.0, dtype=torch.float32):
     _plain("ids", ids, dout.shape[:-1], _IDS, dev)
     dtype = _table_dtype("embed_grad", dtype, dout.dtype)
     ws_bytes = L.wavernn_embed_grad_workspace(n, d, n_rows)
-    ws = _workspace(ws_bytes, dev)
-    out = torch.empty(max(n_rows, 0), d, dtype=dtype, device=dev)
-    _w._check(L.wavernn_embed_grad(dt, _w._ptr(dout), n, d, stride, _w._ptr(ids), _ID_BYTES[ids.dtype], n_rows, scale,
-                                   _DTYPE[dtype], _w._ptr(out), _w._ptr(ws), max(ws_bytes, 0), _w._stream()))
+    ws = _workspace(ws_bytes, dout)
+    out = dout.new_empty((max(n_rows, 0), d), dtype=dtype)
+    _w._check(L.wavernn_embed_grad(dt, _p(dout), n, d, stride, _p(ids), _ID_BYTES[ids.dtype], n_rows, scale,
+                                   _DTYPE[dtype], _p(out), _p(ws), max(ws_bytes, 0), _raw_stream(dev.index)))
     return out
 
 
@@ -213,11 +223,12 @@ def layer_norm(x, gamma=None, beta=None, eps=1e-5, stats=False, out=None):
     _weight("gamma", gamma, d, x)
     _weight("beta", beta, d, x, gamma)
     w = gamma if gamma is not None else beta
-    y, y_stride = _result("out", out, x.shape, x.dtype, dev)
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) if stats else None
-    rstd = torch.empty_like(mean) if stats else None
-    _w._check(L.wavernn_layer_norm(dt, _w._ptr(x), n, d, stride, _w.F32 if w is None else _DTYPE[w.dtype], _w._ptr(gamma),
-                                   _w._ptr(beta), eps, _w._ptr(y), y_stride, _w._ptr(mean), _w._ptr(rstd), _w._stream()))
+    y, y_stride = _result("out", out, x.shape, x.dtype, x)
+    mean = rstd = None
+    if stats:
+        mean, rstd = x.new_empty((2, *x.shape[:-1]), dtype=torch.float32).unbind()
+    _w._check(L.wavernn_layer_norm(dt, _p(x), n, d, stride, _w.F32 if w is None else _DTYPE[w.dtype], _p(gamma),
+                                   _p(beta), eps, _p(y), y_stride, _p(mean), _p(rstd), _raw_stream(dev.index)))
     return (y, mean, rstd) if stats else y
 
 
@@ -233,16 +244,15 @@ def layer_norm_grad(dy, x, mean, rstd, gamma=None, weights=True, out=None):
     for name, t in (("mean", mean), ("rstd", rstd)):
         _plain(name, t, x.shape[:-1], _F32, dev)
     _weight("gamma", gamma, d, x)
-    dx, dx_stride = _result("out", out, x.shape, x.dtype, dev)
+    dx, dx_stride = _result("out", out, x.shape, x.dtype, x)
     dgamma = dbeta = ws = None
     ws_bytes = 0
     if weights:
-        dgamma = torch.empty(d, dtype=torch.float32, device=dev)
-        dbeta = torch.empty(d, dtype=torch.float32, device=dev)
+        dgamma, dbeta = x.new_empty((2, d), dtype=torch.float32).unbind()
         ws_bytes = L.wavernn_layer_norm_grad_workspace(n, d)
-        ws = _workspace(ws_bytes, dev)
-    _w._check(L.wavernn_layer_norm_grad(dt, _w._ptr(dy), _rows("dy", dy)[2], _w._ptr(x), stride, n, d,
-                                        _w.F32 if gamma is None else _DTYPE[gamma.dtype], _w._ptr(gamma), _w._ptr(mean),
-                                        _w._ptr(rstd), _w._ptr(dx), dx_stride, _w._ptr(dgamma), _w._ptr(dbeta),
-                                        _w._ptr(ws), max(ws_bytes, 0), _w._stream()))
+        ws = _workspace(ws_bytes, x)
+    _w._check(L.wavernn_layer_norm_grad(dt, _p(dy), _rows("dy", dy)[2], _p(x), stride, n, d,
+                                        _w.F32 if gamma is None else _DTYPE[gamma.dtype], _p(gamma), _p(mean),
+                                        _p(rstd), _p(dx), dx_stride, _p(dgamma), _p(dbeta),
+                                        _p(ws), max(ws_bytes, 0), _raw_stream(dev.index)))
     return dx, dgamma, dbeta

@@ -33,21 +33,20 @@ __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
     for (int k = 0; k < R; ++k) id[k] = i0 + k < a.n ? wr_id(a.ids, a.id_bytes, i0 + k) : -1;
     for (int c = t * VW; c < a.dim; c += rt * VW) {
       const int count = a.dim - c;
-      float x[R][VW];
+      Raw<T, VW> x[R];
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        if (id[k] >= 0 && id[k] < a.v) load_part<T, VW>((const T*)a.table + id[k] * a.table_stride + c, x[k], count);
-        else
-#pragma unroll
-          for (int i = 0; i < VW; ++i) x[k][i] = 0.0f;
+        const bool in = id[k] >= 0 && id[k] < a.v;
+        x[k] = load_raw<T, VW>((const T*)a.table + (in ? id[k] : 0) * a.table_stride + c, in ? count : 0);
       }
 #pragma unroll
       for (int k = 0; k < R; ++k) {
         if (i0 + k >= a.n) break;
         const float scale = id[k] < 0 ? 0.0f : id[k] < a.v ? a.scale : __builtin_nanf("");
+        float f[VW];
 #pragma unroll
-        for (int i = 0; i < VW; ++i) x[k][i] *= scale;
-        store_part<U, VW>((U*)a.out + (i0 + k) * a.out_stride + c, x[k], count);
+        for (int i = 0; i < VW; ++i) f[i] = (float)x[k][i] * scale;
+        store_part<U, VW>((U*)a.out + (i0 + k) * a.out_stride + c, f, count);
       }
     }
   }
@@ -84,7 +83,8 @@ __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
 #define EG_AHEAD 8
 #define EG_CHUNK_MIN 8      // positions of a chunk: doubled up to 64 while that leaves 1,024 blocks, four a CU (and 64 KiB of LDS are enough)
 #define EG_CHUNK_MAX 64
-#define EG_CLEAR 65536      // bytes that a block clears
+#define EG_CLEAR 16384      // bytes that a block clears at a time
+#define EG_CLEAR_BLOCKS 512
 
 struct EmbedGradArgs {
   const void* dout;
@@ -116,11 +116,15 @@ __device__ __forceinline__ uint32_t sort_key(const EmbedGradArgs& a, int i) {
 // Rank of this lane's digit among the lanes before it that hold the same one, and their base in the wave's
 // counts `cnt`, which grow by this round's.  Lanes without a number pass valid = false.
 __device__ __forceinline__ int wave_rank(uint16_t* cnt, int digit, int bits, bool valid) {
-  uint64_t same = __ballot(valid);
+  const uint64_t on = __ballot(valid);
+  uint32_t lo = (uint32_t)on, hi = (uint32_t)(on >> 32);
   for (int b = 0; b < bits; ++b) {
-    const uint64_t m = __ballot((digit >> b) & 1);
-    same &= (digit >> b) & 1 ? m : ~m;
+    const uint32_t mine = 0u - ((uint32_t)digit >> b & 1u);   // all ones where this lane's bit is set
+    const uint64_t m = __ballot(mine != 0);
+    lo &= ~((uint32_t)m ^ mine);
+    hi &= ~((uint32_t)(m >> 32) ^ mine);
   }
+  const uint64_t same = (uint64_t)hi << 32 | lo;
   const int lane = threadIdx.x & 63, below = __popcll(same & ((1ull << lane) - 1));
   int base = 0;
   if (valid) base = cnt[digit];
@@ -182,12 +186,12 @@ __device__ void clear_part(const EmbedGradArgs& a) {
   }
 }
 
-// All passes by one block, n <= SORT_SMALL.
+// All passes by one block, n <= E SORT_THREADS.
+template <int E>
 __global__ __launch_bounds__(SORT_THREADS) void wr_sort_small_kernel(EmbedGradArgs a) {
-  constexpr int E = SORT_SMALL / SORT_THREADS;
   __shared__ uint16_t cnt[SORT_WAVES][SORT_BINS];
-  __shared__ uint32_t keys[SORT_SMALL];
-  __shared__ uint16_t poss[SORT_SMALL];
+  __shared__ uint32_t keys[E * SORT_THREADS];
+  __shared__ uint16_t poss[E * SORT_THREADS];
   __shared__ uint32_t base[SORT_BINS], tmp[16];
   if ((int)blockIdx.x >= a.sort_blocks) return clear_part(a);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -255,6 +259,17 @@ __global__ __launch_bounds__(SORT_THREADS) void wr_sort_scatter_kernel(EmbedGrad
   if ((int)blockIdx.x >= a.sort_blocks) return clear_part(a);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const uint32_t mask = (1u << a.bits) - 1;
+  uint32_t k[E], p[E];
+  auto read = [&](int64_t i0) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int64_t i = i0 + wave * 64 * E + e * 64 + lane;
+      const bool in = i < a.n;
+      k[e] = in ? (a.src < 0 ? sort_key(a, (int)i) : a.key[a.src][i]) : 0;
+      p[e] = in ? (a.src < 0 ? (uint32_t)i : a.pos[a.src][i]) : 0;
+    }
+  };
+  read((int64_t)blockIdx.x * a.tile);
   {   // this tile's first place of each digit: all smaller digits, and this one in the tiles before
     const int d = tid & (SORT_BINS - 1), half = tid / SORT_BINS;
     uint32_t b = 0, t = 0;
@@ -278,15 +293,8 @@ __global__ __launch_bounds__(SORT_THREADS) void wr_sort_scatter_kernel(EmbedGrad
     if (i0 >= a.n) break;
     for (int i = tid; i < SORT_WAVES * SORT_BINS / 2; i += SORT_THREADS) ((uint32_t*)cnt)[i] = 0;
     __syncthreads();
-    uint32_t k[E], p[E];
+    if (t0 > 0) read(i0);
     int r[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int64_t i = i0 + wave * 64 * E + e * 64 + lane;
-      const bool in = i < a.n;
-      k[e] = in ? (a.src < 0 ? sort_key(a, (int)i) : a.key[a.src][i]) : 0;
-      p[e] = in ? (a.src < 0 ? (uint32_t)i : a.pos[a.src][i]) : 0;
-    }
 #pragma unroll
     for (int e = 0; e < E; ++e)
       r[e] = wave_rank(cnt[wave], (k[e] >> a.shift) & mask, a.bits, i0 + wave * 64 * E + e * 64 + lane < a.n);
@@ -343,11 +351,12 @@ __global__ __launch_bounds__(256) void wr_embed_sum_kernel(EmbedGradArgs a) {
 #pragma unroll
       for (int i = 0; i < VW; ++i) acc[i] = 0.0f;
       for (int p = 0; p < m; p += EG_AHEAD) {
-        float x[EG_AHEAD][VW];
+        Raw<T, VW> x[EG_AHEAD];
 #pragma unroll
-        for (int u = 0; u < EG_AHEAD; ++u)
-          if (p + u < m && key[p + u] < v)
-            load_part<T, VW>((const T*)a.dout + (int64_t)pos[p + u] * a.dout_stride + col, x[u], count);
+        for (int u = 0; u < EG_AHEAD; ++u) {
+          const bool in = p + u < m && key[p + u] < v;
+          x[u] = load_raw<T, VW>((const T*)a.dout + (in ? (int64_t)pos[p + u] : 0) * a.dout_stride + col, in ? count : 0);
+        }
 #pragma unroll
         for (int u = 0; u < EG_AHEAD; ++u) {
           if (p + u >= m) break;
@@ -360,7 +369,7 @@ __global__ __launch_bounds__(256) void wr_embed_sum_kernel(EmbedGradArgs a) {
           }
           if (id < v)
 #pragma unroll
-            for (int i = 0; i < VW; ++i) acc[i] += x[u][i];
+            for (int i = 0; i < VW; ++i) acc[i] += (float)x[u][i];
         }
       }
       flush(cur, true);
@@ -388,14 +397,18 @@ __global__ __launch_bounds__(256) void wr_embed_join_kernel(EmbedGradArgs a) {
     const int64_t col = ((int64_t)blockIdx.y * rt + t) * 4;
     const int count = (int)std::min<int64_t>(4, a.dim - col);
     float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (count > 0)
-#pragma unroll 8
-      for (int64_t j = g; j <= more; j += groups) {
-        float x[4];
-        load_part<float, 4>(a.part + (2 * (c + j) + (j == 0)) * a.dim + col, x, count);
+    for (int64_t j0 = g; j0 <= more; j0 += EG_AHEAD * groups) {
+      Raw<float, 4> x[EG_AHEAD];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += x[i];
+      for (int u = 0; u < EG_AHEAD; ++u) {
+        const int64_t j = j0 + u * groups;
+        x[u] = load_raw<float, 4>(a.part + (2 * (c + (j <= more ? j : 0)) + (j == 0)) * a.dim + col, j <= more ? count : 0);
       }
+#pragma unroll
+      for (int u = 0; u < EG_AHEAD; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] += x[u][i];
+    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) sums[threadIdx.x][i] = acc[i];
@@ -450,11 +463,14 @@ wavernn_status run_embed_grad(EmbedGradArgs& a, void* stream) {
   auto clear = [&](int i) {   // launch i's share of the table, in 16-byte pieces; its blocks
     a.clear0 = bytes / 16 * i / launches * 16;
     a.clear1 = i + 1 == launches ? bytes : bytes / 16 * (i + 1) / launches * 16;
-    return a.sort_blocks + std::min<int64_t>((a.clear1 - a.clear0 + EG_CLEAR - 1) / EG_CLEAR, 1 << 16);
+    // two blocks of 1,024 threads fit a CU: as many as run at once
+    return a.sort_blocks + std::min<int64_t>((a.clear1 - a.clear0 + EG_CLEAR - 1) / EG_CLEAR,
+                                             std::max(EG_CLEAR_BLOCKS - a.sort_blocks, 256));
   };
   if (small) {
     a.sort_blocks = 1;
-    WR_LAUNCH(wr_sort_small_kernel, clear(0), SORT_THREADS, 0, stream, a);
+    if (a.n <= SORT_THREADS) WR_LAUNCH((wr_sort_small_kernel<1>), clear(0), SORT_THREADS, 0, stream, a);
+    else WR_LAUNCH((wr_sort_small_kernel<SORT_SMALL / SORT_THREADS>), clear(0), SORT_THREADS, 0, stream, a);
   } else {
     a.sort_blocks = a.tiles;
     for (int pass = 0; pass < a.passes; ++pass) {

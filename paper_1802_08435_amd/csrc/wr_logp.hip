@@ -223,15 +223,15 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
       continue;
     }
     const T* zr = (const T*)a.logits + row * a.stride;
+    Raw<T, VW> raw[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) raw[e] = load_raw<T, VW>(zr + (e * RT + lane) * VW, a.v - (e * RT + lane) * VW, (T)-__builtin_inff());
     float z[E][VW];
     Soft q{-__builtin_inff(), 0.0f, 0.0f};
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = (e * RT + lane) * VW;
-      load_part<T, VW>(zr + c, z[e], a.v - c, -__builtin_inff());
+    for (int e = 0; e < E; ++e)
 #pragma unroll
-      for (int k = 0; k < VW; ++k) q.m = fmaxf(q.m, z[e][k]);
-    }
+      for (int k = 0; k < VW; ++k) z[e][k] = (float)raw[e][k], q.m = fmaxf(q.m, z[e][k]);
     q.m = group_fmax<RT>(q.m);
     const float base = soft_base(q.m);
 #pragma unroll
@@ -446,22 +446,23 @@ __global__ __launch_bounds__(256) void wr_logp_kernel(LogpArgs a) {
     const int nj = j1 - j0, vecs = (nj + VW - 1) / VW;
     Soft q{-__builtin_inff(), 0.0f, 0.0f};
     for (int i = tid; i < vecs; i += 256 * LW_U) {
-      float z[LW_U][VW], m = q.m;
+      Raw<T, VW> z[LW_U];
+      float m = q.m;
 #pragma unroll
       for (int u = 0; u < LW_U; ++u) {
         const int64_t c = (int64_t)(i + u * 256) * VW;
-        load_part<T, VW>(z0 + c, z[u], i + u * 256 < vecs ? nj - (int)c : 0, -__builtin_inff());
+        z[u] = load_raw<T, VW>(z0 + c, i + u * 256 < vecs ? nj - (int)c : 0, (T)-__builtin_inff());
       }
 #pragma unroll
       for (int u = 0; u < LW_U; ++u)
 #pragma unroll
-        for (int k = 0; k < VW; ++k) m = fmaxf(m, z[u][k]);
+        for (int k = 0; k < VW; ++k) m = fmaxf(m, (float)z[u][k]);
       if (m > q.m) q = soft_at(q, m);
       const float base = soft_base(m);
 #pragma unroll
       for (int u = 0; u < LW_U; ++u)
 #pragma unroll
-        for (int k = 0; k < VW; ++k) soft_term(z[u][k], base, q.s, q.w);
+        for (int k = 0; k < VW; ++k) soft_term((float)z[u][k], base, q.s, q.w);
     }
     const float best = q.m;
     const bool nan = q.s != q.s;
@@ -557,6 +558,13 @@ __global__ __launch_bounds__(256) void wr_logp_grad_kernel(LogpGradArgs a) {
     const int64_t t = row_token(a.f, row);
     const T* z = (const T*)a.f.logits + row * a.f.stride;
     T* dz = (T*)a.dlogits + row * a.dstride;
+    Raw<T, VW> raw[LG_U];
+    const int64_t i0 = ((int64_t)seg * LG_U * rt + t0) * VW;
+#pragma unroll
+    for (int u = 0; u < LG_U; ++u) {
+      const int64_t j = i0 + (int64_t)u * rt * VW;
+      raw[u] = load_raw<T, VW>(z + j, t < 0 || j >= v ? 0 : (int)(v - j));
+    }
     const float lse = t < 0 ? 0.0f : a.lse_in[row];
     const bool zero = t < 0 || lse == -__builtin_inff();   // padding, or every class masked
     const float gl = a.g_logp && !zero ? a.g_logp[row] : 0.0f;
@@ -568,34 +576,30 @@ __global__ __launch_bounds__(256) void wr_logp_grad_kernel(LogpGradArgs a) {
     if (!zero)
       for (int k = 0; k < a.f.top; ++k)
         if (ti[k] >= 0) gp -= tg[k];
-    float x[LG_U][VW];
-    const int64_t i0 = ((int64_t)seg * LG_U * rt + t0) * VW;
-#pragma unroll
-    for (int u = 0; u < LG_U; ++u) {
-      const int64_t j = i0 + (int64_t)u * rt * VW;
-      load_part<T, VW>(z + j, x[u], zero || j >= v ? 0 : (int)(v - j));
-    }
 #pragma unroll
     for (int u = 0; u < LG_U; ++u) {
       const int64_t j = i0 + (int64_t)u * rt * VW;
       if (j >= v) break;
+      float x[VW];
+#pragma unroll
+      for (int k = 0; k < VW; ++k) x[k] = zero ? 0.0f : (float)raw[u][k];
       if (!zero) {
 #pragma unroll
         for (int k = 0; k < VW; ++k) {
-          const float lp = x[u][k] - lse;
-          x[u][k] = fexp(lp) * (gp - gh * (fmaxf(lp, WR_FAR) + h));
+          const float lp = x[k] - lse;
+          x[k] = fexp(lp) * (gp - gh * (fmaxf(lp, WR_FAR) + h));
         }
         if (t >= j && t < j + VW)
 #pragma unroll
           for (int k = 0; k < VW; ++k)
-            if (t == j + k) x[u][k] += gl;
+            if (t == j + k) x[k] += gl;
         for (int i = 0; i < a.f.top; ++i)
           if (ti[i] >= j && ti[i] < j + VW)
 #pragma unroll
             for (int k = 0; k < VW; ++k)
-              if (ti[i] == j + k) x[u][k] += tg[i];
+              if (ti[i] == j + k) x[k] += tg[i];
       }
-      store_part<T, VW>(dz + j, x[u], (int)(v - j));
+      store_part<T, VW>(dz + j, x, (int)(v - j));
     }
   }
 }

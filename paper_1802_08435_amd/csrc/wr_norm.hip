@@ -69,28 +69,26 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_kernel(NormArgs a
   __shared__ float red[2][BT / 64];
   const int t = threadIdx.x % RT;
   const float inv_d = 1.0f / (float)a.d;
-  float ga[E][VW], be[E][VW];
+  Raw<W, VW> ga[E], be[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int c = (e * RT + t) * VW;
-#pragma unroll
-    for (int i = 0; i < VW; ++i) ga[e][i] = 1.0f, be[e][i] = 0.0f;
-    if (a.gamma) load_part<W, VW>((const W*)a.gamma + c, ga[e], a.d - c);
-    if (a.beta) load_part<W, VW>((const W*)a.beta + c, be[e], a.d - c);
+    ga[e] = load_raw<W, VW>((const W*)a.gamma + c, a.gamma ? a.d - c : 0, (W)1.0f);
+    be[e] = load_raw<W, VW>((const W*)a.beta + c, a.beta ? a.d - c : 0);
   }
   for (int64_t i0 = (int64_t)blockIdx.x * G; i0 < a.n; i0 += (int64_t)gridDim.x * G) {
     const int64_t i = i0 + threadIdx.x / RT;
     const bool on = i < a.n;   // (only the last rows of a block that shares rows; its sums stay in the group)
     const T* x = (const T*)a.x + i * a.x_stride;
     T* y = (T*)a.y + i * a.y_stride;
+    Raw<T, VW> raw[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) raw[e] = load_raw<T, VW>(x + (e * RT + t) * VW, on ? a.d - (e * RT + t) * VW : 0);
     float v[E][VW], s[1] = {0.0f};
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = (e * RT + t) * VW;
-      load_part<T, VW>(x + c, v[e], on ? a.d - c : 0);
+    for (int e = 0; e < E; ++e)
 #pragma unroll
-      for (int k = 0; k < VW; ++k) s[0] += v[e][k];
-    }
+      for (int k = 0; k < VW; ++k) v[e][k] = (float)raw[e][k], s[0] += v[e][k];
     row_sums<RT, 1>(s, red[0]);
     const float m = s[0] * inv_d;
     s[0] = 0.0f;
@@ -110,7 +108,7 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_kernel(NormArgs a
       for (int e = 0; e < E; ++e) {
         const int c = (e * RT + t) * VW;
 #pragma unroll
-        for (int k = 0; k < VW; ++k) v[e][k] = __builtin_fmaf(v[e][k] * r, ga[e][k], be[e][k]);
+        for (int k = 0; k < VW; ++k) v[e][k] = __builtin_fmaf(v[e][k] * r, (float)ga[e][k], (float)be[e][k]);
         store_part<T, VW>(y + c, v[e], a.d - c);
       }
       if (t == 0) {
@@ -139,9 +137,10 @@ __global__ __launch_bounds__(1024) void wr_norm_wide_kernel(NormArgs a) {
     const float m = s[0] / (float)a.d;
     s[0] = 0.0f;
     for (int64_t c = threadIdx.x * VW; c < a.d; c += RT * VW) {
-      load_part<T, VW>(x + c, v, (int)(a.d - c), m);
+      load_part<T, VW>(x + c, v, (int)(a.d - c));
 #pragma unroll
-      for (int k = 0; k < VW; ++k) s[0] = __builtin_fmaf(v[k] - m, v[k] - m, s[0]);
+      for (int k = 0; k < VW; ++k)
+        if (c + k < a.d) s[0] = __builtin_fmaf(v[k] - m, v[k] - m, s[0]);
     }
     row_sums<RT, 1>(s, red[1]);
     const float r = 1.0f / sqrtf(s[0] / (float)a.d + a.eps);
@@ -184,36 +183,39 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_grad_kernel(NormG
   __shared__ float red[2][BT / 64 * 2];
   const int t = threadIdx.x % RT;
   const float inv_d = 1.0f / (float)a.d;
-  float ga[E][VW], dg[E][VW], db[E][VW];
+  Raw<W, VW> ga[E];
+  float dg[E][VW], db[E][VW];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int c = (e * RT + t) * VW;
+    ga[e] = load_raw<W, VW>((const W*)a.gamma + c, a.gamma ? a.d - c : 0, (W)1.0f);
 #pragma unroll
-    for (int k = 0; k < VW; ++k) ga[e][k] = 1.0f, dg[e][k] = db[e][k] = 0.0f;
-    if (a.gamma) load_part<W, VW>((const W*)a.gamma + c, ga[e], a.d - c);
+    for (int k = 0; k < VW; ++k) dg[e][k] = db[e][k] = 0.0f;
   }
   int turn = 0;
   for (int64_t i0 = (int64_t)blockIdx.x * G; i0 < a.n; i0 += (int64_t)gridDim.x * G, turn ^= 1) {
     const int64_t i = i0 + threadIdx.x / RT;
     const bool on = i < a.n;
-    const float m = on ? a.mean[i] : 0.0f, r = on ? a.rstd[i] : 0.0f;
-    float h[E][VW], g[E][VW], s[2] = {0.0f, 0.0f};
+    Raw<T, VW> rx[E], ry[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int c = (e * RT + t) * VW, count = on ? a.d - c : 0;
-      load_part<T, VW>((const T*)a.x + i * a.x_stride + c, h[e], count, m);   // (past the row: h = 0, dy = 0)
-      load_part<T, VW>((const T*)a.dy + i * a.dy_stride + c, g[e], count);
+      rx[e] = load_raw<T, VW>((const T*)a.x + i * a.x_stride + c, count);
+      ry[e] = load_raw<T, VW>((const T*)a.dy + i * a.dy_stride + c, count);   // (past the row 0: no part of any sum)
     }
+    const float m = on ? a.mean[i] : 0.0f, r = on ? a.rstd[i] : 0.0f;
+    float h[E][VW], g[E][VW], s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int e = 0; e < E; ++e)
 #pragma unroll
       for (int k = 0; k < VW; ++k) {
-        h[e][k] = (h[e][k] - m) * r;
+        h[e][k] = ((float)rx[e][k] - m) * r;
+        g[e][k] = (float)ry[e][k];
         if constexpr (WG) {
           dg[e][k] = __builtin_fmaf(g[e][k], h[e][k], dg[e][k]);
           db[e][k] += g[e][k];
         }
-        g[e][k] *= ga[e][k];
+        g[e][k] *= (float)ga[e][k];
         s[0] += g[e][k];
         s[1] = __builtin_fmaf(g[e][k], h[e][k], s[1]);
       }
@@ -274,7 +276,7 @@ __global__ __launch_bounds__(1024) void wr_norm_grad_wide_kernel(NormGradArgs a)
 #pragma unroll
       for (int k = 0; k < VW; ++k) ga[k] = 1.0f;
       if (a.gamma) load_part<W, VW>((const W*)a.gamma + c, ga, count);
-      load_part<T, VW>(x + c, h, count, m);
+      load_part<T, VW>(x + c, h, count);
       load_part<T, VW>(dy + c, g, count);
 #pragma unroll
       for (int k = 0; k < VW; ++k) h[k] = (h[k] - m) * r, g[k] *= ga[k];
@@ -305,7 +307,7 @@ __global__ __launch_bounds__(256) void wr_norm_wide_dw_kernel(NormGradArgs a) {
 #pragma unroll 4
   for (int64_t i = blockIdx.y; i < a.n; i += gridDim.y) {
     const float m = a.mean[i], r = a.rstd[i];
-    load_part<T, 4>((const T*)a.x + i * a.x_stride + c, x, count, m);
+    load_part<T, 4>((const T*)a.x + i * a.x_stride + c, x, count);
     load_part<T, 4>((const T*)a.dy + i * a.dy_stride + c, dy, count);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {

@@ -53,28 +53,44 @@ __device__ __forceinline__ int64_t wr_id(const void* ids, int bytes, int64_t i) 
 // N adjacent elements from or to any address aligned to an element: whole
 // vectors as one access (the hardware takes them at any alignment; at an odd
 // one an access touches two cache lines now and then), the first `count` of a
-// row's last vector one by one.
+// row's last vector one by one.  load_raw leaves the elements as they are, with
+// `fill` past the count, so that the loads of several vectors are under way
+// before the first is waited for: a conversion right behind a load that not every lane
+// makes would wait for it there.
 template <class T, int N>
-__device__ __forceinline__ void load_vec(const T* p, float (&f)[N]) {
-  typedef T vec __attribute__((ext_vector_type(N)));
-  vec x;
-  __builtin_memcpy(&x, p, sizeof x);
+struct RawVec {
+  typedef T type __attribute__((ext_vector_type(N)));
+};
+template <class T, int N>
+using Raw = typename RawVec<T, N>::type;
+template <class T, int N>
+__device__ __forceinline__ Raw<T, N> load_raw(const T* p, int count, T fill = (T)0.0f) {
+  Raw<T, N> x;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = fill;
+  if (count >= N) {
+    __builtin_memcpy(&x, p, sizeof x);
+  } else if (count > 0) {
+    T y[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = p[i < count ? i : count - 1];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = i < count ? y[i] : fill;
+  }
+  return x;
+}
+template <class T, int N>
+__device__ __forceinline__ void load_part(const T* p, float (&f)[N], int count) {
+  const Raw<T, N> x = load_raw<T, N>(p, count);
 #pragma unroll
   for (int i = 0; i < N; ++i) f[i] = (float)x[i];
 }
 template <class T, int N>
 __device__ __forceinline__ void store_vec(T* p, const float (&f)[N]) {
-  typedef T vec __attribute__((ext_vector_type(N)));
-  vec x;
+  Raw<T, N> x;
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = (T)f[i];
   __builtin_memcpy(p, &x, sizeof x);
-}
-template <class T, int N>
-__device__ __forceinline__ void load_part(const T* p, float (&f)[N], int count, float rest = 0.0f) {
-  if (count >= N) return load_vec<T, N>(p, f);
-#pragma unroll
-  for (int i = 0; i < N; ++i) f[i] = i < count ? (float)p[i] : rest;
 }
 template <class T, int N>
 __device__ __forceinline__ void store_part(T* p, const float (&f)[N], int count) {

@@ -43,22 +43,21 @@ __device__ __forceinline__ int64_t row_out(const LogpArgs& a, int64_t row) {
   }
 }
 
-// Order of the alternatives as whole numbers: a logit's rank in the upper half
-// (NaN above all, -0 equal to +0), its number complemented in the lower, so
-// that no two classes compare equal.
-__device__ __forceinline__ u64 top_key(float z, int j) {
-  uint32_t u = __float_as_uint(z + 0.0f);
-  u = z != z ? 0xfffffffeu : (u >> 31) ? ~u : u | 0x80000000u;
-  return (u64)u << 32 | (uint32_t)~j;
+// Order of the alternatives as whole numbers: a logit's rank (its bits with the sign turned
+// round, -0 as +0, every NaN as the one above +inf) in the upper half, its number complemented in the
+// lower, so that no two classes compare equal.  0 is below every logit.
+__device__ __forceinline__ float plain_nan(float z) { return z != z ? __builtin_nanf("") : z; }
+__device__ __forceinline__ uint32_t rank_of(float z) {   // z not NaN, or plain_nan's
+  const int u = (int)__float_as_uint(z + 0.0f);
+  return (uint32_t)(u ^ (u >> 31 | (int)0x80000000));
 }
+__device__ __forceinline__ uint32_t top_rank(float z) { return rank_of(plain_nan(z)); }
+__device__ __forceinline__ u64 top_key(float z, int j) { return (u64)top_rank(z) << 32 | (uint32_t)~j; }
 __device__ __forceinline__ float key_value(u64 k) {
   const uint32_t u = (uint32_t)(k >> 32);
-  return __uint_as_float(u == 0xfffffffeu ? 0x7fc00000u : (u >> 31) ? u & 0x7fffffffu : ~u);
+  return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u);
 }
 __device__ __forceinline__ int key_class(u64 k) { return (int)~(uint32_t)k; }
-
-// Order of the logits alone, as top_key's upper half; 0 is below every logit.
-__device__ __forceinline__ uint32_t top_rank(float z) { return (uint32_t)(top_key(z, 0) >> 32); }
 
 // Running maximum, sum of e^(z - m) and sum of (z - m) e^(z - m).
 struct Soft {
@@ -141,21 +140,21 @@ __device__ __forceinline__ uint32_t group_umin(uint32_t v) {
   return (uint32_t)group_reduce<RT>((int)v, [](int a, int b) { return (int)((uint32_t)a < (uint32_t)b ? (uint32_t)a : (uint32_t)b); });
 }
 
-// One vector's classes c, c + 1, ... in the order of the alternatives; ones past the row's v
-// classes come last, with key 0.  pop() takes the first away.
+// One vector's classes c, c + 1, ... in the order of the alternatives (NaN as plain_nan's).  The ones past the
+// row are -inf with numbers past every other, and so come last.  pop() takes the first away.
 template <class T>
 struct TopVec {   // 16-bit logits: rank and number in one word, all different, sorted by a merge network (Batcher, 1968)
   uint32_t key[8];
-  __device__ __forceinline__ void init(const float (&z)[8], int c, int v) {
+  __device__ __forceinline__ void init(const float (&z)[8], int c) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       uint32_t u;
-      if constexpr (__is_same(T, __bf16)) u = top_rank(z[k]) >> 16;   // a bf16's bits are a float's upper half
+      if constexpr (__is_same(T, __bf16)) u = rank_of(z[k]) & 0xffff0000u;   // a bf16's bits are a float's upper half
       else {
-        const uint32_t h = __builtin_bit_cast(uint16_t, (_Float16)(z[k] + 0.0f));
-        u = z[k] != z[k] ? 0xffffu : (h >> 15) ? ~h & 0xffffu : h | 0x8000u;
+        const int h = (int)__builtin_bit_cast(uint16_t, (_Float16)(z[k] + 0.0f)) << 16;
+        u = (uint32_t)(h ^ (h >> 31 | (int)0x80000000)) & 0xffff0000u;
       }
-      key[k] = c + k < v ? u << 16 | (uint32_t)(0xffff - (c + k)) : 0;
+      key[k] = u | (uint32_t)(0xffff - (c + k));
     }
     constexpr int net[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
                                 {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
@@ -176,16 +175,15 @@ struct TopVec {   // 16-bit logits: rank and number in one word, all different, 
   static __device__ __forceinline__ float value(uint32_t key) {
     if constexpr (__is_same(T, __bf16)) return key_value((u64)(key & 0xffff0000u) << 32 | ((key >> 31) ? 0ull : 0xffffull << 32));
     const uint32_t u = key >> 16;
-    return u == 0xffffu ? __builtin_nanf("")
-                        : (float)__builtin_bit_cast(_Float16, (uint16_t)((u >> 15) ? u & 0x7fffu : ~u));
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)((u >> 15) ? u & 0x7fffu : ~u));
   }
 };
 template <>
 struct TopVec<float> {   // sorted by neighbours' exchanges, which keep equal logits in their order
   uint32_t key[4], k_[4];
-  __device__ __forceinline__ void init(const float (&z)[4], int c, int v) {
+  __device__ __forceinline__ void init(const float (&z)[4], int) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) key[k] = c + k < v ? top_rank(z[k]) : 0, k_[k] = k;
+    for (int k = 0; k < 4; ++k) key[k] = rank_of(z[k]), k_[k] = k;
     constexpr int net[6] = {0, 2, 1, 0, 2, 1};
 #pragma unroll
     for (int i = 0; i < 6; ++i) {
@@ -245,7 +243,12 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
     if (a.top == 0) continue;
     TopVec<T> vec[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) vec[e].init(z[e], (e * RT + lane) * VW, a.v);
+    for (int e = 0; e < E; ++e) {
+      if (q.s != q.s)
+#pragma unroll
+        for (int k = 0; k < VW; ++k) z[e][k] = plain_nan(z[e][k]);
+      vec[e].init(z[e], (e * RT + lane) * VW);
+    }
     uint32_t won[KR] = {}, won_at[KR] = {};
     for (int i = 0; i < a.top; ++i) {
       uint32_t best = vec[0].key[0], at = vec[0].at(lane * VW);

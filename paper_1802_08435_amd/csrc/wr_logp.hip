@@ -105,7 +105,7 @@ __device__ __forceinline__ void put_padding(const LogpArgs& a, int64_t o, int i)
 
 // ---- a group of lanes a row ----------------------------------------------------
 // Reductions over RT = 16 lanes by rotations within a row of 16 (every lane gets the result, in the same bits, as
-// each step only exchanges the operands of a commutative operation), over 64 by joining the four rows' results.
+// each step only exchanges the operands of a commutative operation), over 32 and 64 by joining the rows' results.
 template <int N>
 __device__ __forceinline__ int rotate16(int v) { return __builtin_amdgcn_update_dpp(0, v, 0x120 + N, 0xf, 0xf, true); }
 template <int RT, class F>
@@ -114,6 +114,7 @@ __device__ __forceinline__ int group_reduce(int v, F f) {
   v = f(v, rotate16<4>(v));
   v = f(v, rotate16<2>(v));
   v = f(v, rotate16<1>(v));
+  if constexpr (RT == 32) v = f(v, __shfl_xor(v, 16, 64));
   if constexpr (RT == 64)
     v = f(f(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
           f(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
@@ -316,7 +317,13 @@ __device__ __forceinline__ void put_ranked(const LogpArgs& a, LogpShared& sh, in
   for (int i = threadIdx.x; i < n; i += 256) {
     const u64 key = sh.list[i];
     int r = 0;
-    for (int j = 0; j < n; ++j) r += sh.list[j] > key;
+    for (int j0 = 0; j0 < n; j0 += 8) {   // (eight reads under way together; LW_CAP is a multiple of 8)
+      u64 x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = sh.list[j0 + j];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r += j0 + j < n && x[j] > key;
+    }
     if (r < a.top) put_top(a, o, part, r, key, sub);
   }
 }
@@ -525,9 +532,11 @@ __global__ __launch_bounds__(256) void wr_logp_join_kernel(LogpArgs a) {
     __syncthreads();
     if (a.splits >= a.top) {
       if (tid < a.splits) {
+        const u64 mine = sh.list[tid];
         int r = 0;
-        for (int j = 0; j < a.splits; ++j) r += sh.list[j] > sh.list[tid];
-        if (r == a.top - 1) sh.wave_best[0] = sh.list[tid];
+#pragma unroll 8
+        for (int j = 0; j < a.splits; ++j) r += sh.list[j] > mine;
+        if (r == a.top - 1) sh.wave_best[0] = mine;
       }
       __syncthreads();
       low = sh.wave_best[0];
@@ -635,8 +644,11 @@ static wavernn_status logp_launch(LogpArgs& a, void* stream) {
   const int vecs = (int)(((int64_t)a.v + VW - 1) / VW);
   auto blocks = [&](int rows) { return std::min<int64_t>((a.n + rows - 1) / rows, LOGP_BLOCKS); };
   if (vecs <= 16) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 1>), blocks(16), 256, 0, stream, a);
+  else if (vecs <= 32) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 2>), blocks(16), 256, 0, stream, a);
   else if (vecs <= 64) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 4>), blocks(16), 256, 0, stream, a);
+  else if (vecs <= 128) WR_LAUNCH((wr_logp_rows_kernel<T, 32, 4>), blocks(8), 256, 0, stream, a);
   else if (vecs <= 256) WR_LAUNCH((wr_logp_rows_kernel<T, 64, 4>), blocks(4), 256, 0, stream, a);
+  else if (vecs <= 512) WR_LAUNCH((wr_logp_rows_kernel<T, 64, 8>), blocks(4), 256, 0, stream, a);
   else {
     a.splits = a.part ? logp_splits(a.n, a.v) : 1;
     a.seg = (int)(((int64_t)a.v + a.splits - 1) / a.splits + 7) / 8 * 8;

@@ -31,8 +31,8 @@ __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
     int64_t id[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) id[k] = i0 + k < a.n ? wr_id(a.ids, a.id_bytes, i0 + k) : -1;
-    for (int c = t * VW; c < a.dim; c += rt * VW) {
-      const int count = a.dim - c;
+    for (int c0 = t * VW; c0 < a.dim; c0 += rt * VW) {
+      const int c = a.dim < VW ? 0 : vec_begin<VW>(c0, a.dim), count = a.dim - c;
       Raw<T, VW> x[R];
 #pragma unroll
       for (int k = 0; k < R; ++k) {
@@ -95,13 +95,14 @@ struct EmbedGradArgs {
   int v;
   float scale;
   void* dtable;
+  bool few;                     // few rows: no sort; tiles segments of `tile` ids
   int passes, bits;             // of the sort
   int tiles, tile;              // of the sort's launches; ids of a tile (a multiple of SORT_TILE)
   uint32_t *key[2], *pos[2];    // [n] each; [1] absent with n <= SORT_SMALL
   uint32_t* hist;               // [tiles][SORT_BINS]
   int src, shift;               // of one pass: buffer read (-1: the ids), digit's lowest bit
   const uint32_t *skey, *spos;  // sorted
-  float* part;                  // [chunks][2][dim]
+  float* part;                  // [chunks][2][dim]; few rows: [tiles][v][dim]
   int chunk, chunks;            // positions of a chunk
   int row_threads;              // threads on a row (256 / row_threads chunks a block)
   int sort_blocks;              // of a sort's launch; the ones behind them clear bytes clear0 .. clear1 of dtable
@@ -334,8 +335,8 @@ __global__ __launch_bounds__(256) void wr_embed_sum_kernel(EmbedGradArgs a) {
     const uint32_t *key = at + l0, *pos = at + per + l0;
     const uint32_t first = key[0], last = key[m - 1], v = (uint32_t)a.v;
     const bool from = p0 > 0 && a.skey[p0 - 1] == first, on = p0 + m < a.n && a.skey[p0 + m] == last;
-    for (int col = t * VW; col < a.dim; col += rt * VW) {
-      const int count = a.dim - col;
+    for (int c0 = t * VW; c0 < a.dim; c0 += rt * VW) {
+      const int col = a.dim < VW ? 0 : vec_begin<VW>(c0, a.dim), count = a.dim - col;
       float acc[VW];
       uint32_t cur = first;
       auto flush = [&](uint32_t id, bool at_end) {
@@ -424,8 +425,108 @@ __global__ __launch_bounds__(256) void wr_embed_join_kernel(EmbedGradArgs a) {
   }
 }
 
+// ---- few rows ----------------------------------------------------------------
+// A table of up to EF_ROWS rows (bytes, labels): block (v, s) looks for number v among the ids of segment s
+// itself, which takes no sort, and sums the rows it finds; with several segments one more launch adds
+// their sums in order.  12,800 rows of 64 into 97: 22 us by the sort (four launches), EF_TIME.
+#define EF_ROWS 256
+#define EF_SEG 2048        // ids of a segment: 8 a thread; more (up to 8,192) past 64 segments
+#define EF_SEG_MAX 8192
+#define EF_SEGS 64
+
+template <class T, class U>
+__global__ __launch_bounds__(256) void wr_embed_few_kernel(EmbedGradArgs a) {
+  constexpr int VW = vec_of<T, U>();
+  __shared__ uint16_t found[EF_SEG_MAX];   // each wave's hits, in order, in its quarter of the segment
+  __shared__ int hits[4];
+  __shared__ float sums[256][VW + 1];      // (padded against bank conflicts)
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, v = blockIdx.x;
+  const int64_t i0 = (int64_t)blockIdx.y * a.tile;
+  const int quarter = a.tile / 4;
+  int n = 0;
+  for (int j = 0; j < quarter; j += 64) {
+    const int64_t i = i0 + wave * quarter + j + lane;
+    const bool hit = i < a.n && wr_id(a.ids, a.id_bytes, i) == v;
+    const uint64_t m = __ballot(hit);
+    if (hit) found[wave * quarter + n + __popcll(m & ((1ull << lane) - 1))] = (uint16_t)(wave * quarter + j + lane);
+    n += __popcll(m);
+  }
+  if (lane == 0) hits[wave] = n;
+  __syncthreads();
+  const int h0 = hits[0], h1 = h0 + hits[1], h2 = h1 + hits[2], total = h2 + hits[3];
+  const int rt = a.row_threads, groups = 256 / rt, g = tid / rt, t = tid % rt;
+  for (int b0 = 0; b0 < a.dim; b0 += rt * VW) {
+    const int c0 = b0 + t * VW, col = a.dim < VW ? 0 : vec_begin<VW>(c0, a.dim), count = c0 < a.dim ? a.dim - col : 0;
+    float acc[VW];
+#pragma unroll
+    for (int k = 0; k < VW; ++k) acc[k] = 0.0f;
+    for (int j0 = g; j0 < total; j0 += EG_AHEAD * groups) {
+      Raw<T, VW> x[EG_AHEAD];
+#pragma unroll
+      for (int u = 0; u < EG_AHEAD; ++u) {
+        const int j = j0 + u * groups;
+        const int q = j < h0 ? j : j < h1 ? quarter + j - h0 : j < h2 ? 2 * quarter + j - h1 : 3 * quarter + j - h2;
+        x[u] = load_raw<T, VW>((const T*)a.dout + (j < total ? i0 + found[q] : 0) * a.dout_stride + col, j < total ? count : 0);
+      }
+#pragma unroll
+      for (int u = 0; u < EG_AHEAD; ++u)
+#pragma unroll
+        for (int k = 0; k < VW; ++k) acc[k] += (float)x[u][k];
+    }
+    if (groups > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < VW; ++k) sums[tid][k] = acc[k];
+      __syncthreads();
+      if (g == 0)
+        for (int q = 1; q < groups; ++q)
+#pragma unroll
+          for (int k = 0; k < VW; ++k) acc[k] += sums[q * rt + t][k];
+    }
+    if (g == 0 && count > 0) {
+      if (a.tiles > 1) {
+        store_part<float, VW>(a.part + ((int64_t)blockIdx.y * a.v + v) * a.dim + col, acc, count);
+      } else {
+#pragma unroll
+        for (int k = 0; k < VW; ++k) acc[k] *= a.scale;
+        store_part<U, VW>((U*)a.dtable + (int64_t)v * a.dim + col, acc, count);
+      }
+    }
+  }
+}
+
+template <class U>
+__global__ __launch_bounds__(256) void wr_embed_few_join_kernel(EmbedGradArgs a) {
+  const int64_t cells = (int64_t)a.v * a.dim;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < cells; i += (int64_t)gridDim.x * 1024) {
+    const int count = (int)std::min<int64_t>(4, cells - i);
+    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = 0; s0 < a.tiles; s0 += EG_AHEAD) {
+      Raw<float, 4> x[EG_AHEAD];
+#pragma unroll
+      for (int u = 0; u < EG_AHEAD; ++u)
+        x[u] = load_raw<float, 4>(a.part + (s0 + u < a.tiles ? s0 + u : 0) * cells + i, s0 + u < a.tiles ? count : 0);
+#pragma unroll
+      for (int u = 0; u < EG_AHEAD; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[k] += x[u][k];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[k] *= a.scale;
+    store_part<U, 4>((U*)a.dtable + i, acc, count);
+  }
+}
+
 // Sizes of a call and its workspace's layout; returns the workspace's bytes.
 int64_t plan_embed_grad(int64_t n, int32_t dim, int64_t v, EmbedGradArgs* a, unsigned char* ws) {
+  a->few = v <= EF_ROWS && n <= (int64_t)EF_SEGS * EF_SEG_MAX;
+  if (a->few) {
+    a->tile = EF_SEG;
+    while (n > (int64_t)EF_SEGS * a->tile) a->tile *= 2;
+    a->tiles = (int)std::max<int64_t>(1, (n + a->tile - 1) / a->tile);
+    a->part = (float*)ws;
+    return a->tiles > 1 ? (int64_t)4 * a->tiles * v * dim : 0;
+  }
   int bits = 1;
   while (bits < 32 && (v >> bits)) ++bits;   // keys 0 .. v
   a->passes = (bits + SORT_BITS - 1) / SORT_BITS;
@@ -456,6 +557,17 @@ int64_t plan_embed_grad(int64_t n, int32_t dim, int64_t v, EmbedGradArgs* a, uns
 
 template <class T, class U>
 wavernn_status run_embed_grad(EmbedGradArgs& a, void* stream) {
+  if (a.few) {
+    constexpr int VW = vec_of<T, U>();
+    a.row_threads = wr_row_threads(((int64_t)a.dim + VW - 1) / VW);
+    void* argv[] = {&a};
+    const hipError_t e = hipLaunchKernel((const void*)wr_embed_few_kernel<T, U>, dim3(a.v, a.tiles), dim3(256), argv, 0,
+                                         (hipStream_t)stream);
+    if (e != hipSuccess) return wr_fail(WAVERNN_E_HIP, "launch of wr_embed_few_kernel: %s", hipGetErrorString(e));
+    if (a.tiles > 1)
+      WR_LAUNCH((wr_embed_few_join_kernel<U>), std::min<int64_t>(((int64_t)a.v * a.dim + 1023) / 1024, 1 << 16), 256, 0, stream, a);
+    return WAVERNN_OK;
+  }
   int last = 0;
   const bool small = a.n <= SORT_SMALL;
   const int launches = small ? 1 : 2 * a.passes;

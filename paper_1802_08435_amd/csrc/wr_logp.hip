@@ -142,11 +142,12 @@ __device__ __forceinline__ uint32_t group_umin(uint32_t v) {
 }
 
 // One vector's classes c, c + 1, ... in the order of the alternatives (NaN as plain_nan's).  The ones past the
-// row are -inf with numbers past every other, and so come last.  pop() takes the first away.
+// row are -inf with numbers past every other, and so come last; ones below `own` are another vector's
+// (key 0).  pop() takes the first away.
 template <class T>
 struct TopVec {   // 16-bit logits: rank and number in one word, all different, sorted by a merge network (Batcher, 1968)
   uint32_t key[8];
-  __device__ __forceinline__ void init(const float (&z)[8], int c) {
+  __device__ __forceinline__ void init(const float (&z)[8], int c, int own) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       uint32_t u;
@@ -157,6 +158,10 @@ struct TopVec {   // 16-bit logits: rank and number in one word, all different, 
       }
       key[k] = u | (uint32_t)(0xffff - (c + k));
     }
+    if (c < own)
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (c + k < own) key[k] = 0;
     constexpr int net[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
                                 {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
 #pragma unroll
@@ -182,9 +187,13 @@ struct TopVec {   // 16-bit logits: rank and number in one word, all different, 
 template <>
 struct TopVec<float> {   // sorted by neighbours' exchanges, which keep equal logits in their order
   uint32_t key[4], k_[4];
-  __device__ __forceinline__ void init(const float (&z)[4], int) {
+  __device__ __forceinline__ void init(const float (&z)[4], int c, int own) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) key[k] = rank_of(z[k]), k_[k] = k;
+    if (c < own)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < own) key[k] = 0;
     constexpr int net[6] = {0, 2, 1, 0, 2, 1};
 #pragma unroll
     for (int i = 0; i < 6; ++i) {
@@ -223,14 +232,26 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
     }
     const T* zr = (const T*)a.logits + row * a.stride;
     Raw<T, VW> raw[E];
+    int c[E];   // the first class of each vector; a row's last one may begin with another lane's classes
 #pragma unroll
-    for (int e = 0; e < E; ++e) raw[e] = load_raw<T, VW>(zr + (e * RT + lane) * VW, a.v - (e * RT + lane) * VW, (T)-__builtin_inff());
+    for (int e = 0; e < E; ++e) {
+      const int c0 = (e * RT + lane) * VW;
+      c[e] = a.v < VW || c0 >= a.v ? c0 : vec_begin<VW>(c0, a.v);
+      raw[e] = load_raw<T, VW>(zr + c[e], a.v - c[e], (T)-__builtin_inff());
+    }
     float z[E][VW];
     Soft q{-__builtin_inff(), 0.0f, 0.0f};
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int e = 0; e < E; ++e) {
 #pragma unroll
-      for (int k = 0; k < VW; ++k) z[e][k] = (float)raw[e][k], q.m = fmaxf(q.m, z[e][k]);
+      for (int k = 0; k < VW; ++k) z[e][k] = (float)raw[e][k];
+      if (c[e] < (e * RT + lane) * VW)   // (no lane of most waves)
+#pragma unroll
+        for (int k = 0; k < VW; ++k)
+          if (c[e] + k < (e * RT + lane) * VW) z[e][k] = -__builtin_inff();
+#pragma unroll
+      for (int k = 0; k < VW; ++k) q.m = fmaxf(q.m, z[e][k]);
+    }
     q.m = group_fmax<RT>(q.m);
     const float base = soft_base(q.m);
 #pragma unroll
@@ -248,16 +269,16 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
       if (q.s != q.s)
 #pragma unroll
         for (int k = 0; k < VW; ++k) z[e][k] = plain_nan(z[e][k]);
-      vec[e].init(z[e], (e * RT + lane) * VW);
+      vec[e].init(z[e], c[e], (e * RT + lane) * VW);
     }
     uint32_t won[KR] = {}, won_at[KR] = {};
     for (int i = 0; i < a.top; ++i) {
-      uint32_t best = vec[0].key[0], at = vec[0].at(lane * VW);
+      uint32_t best = vec[0].key[0], at = vec[0].at(c[0]);
 #pragma unroll
       for (int e = 1; e < E; ++e) {
         const bool more = vec[e].key[0] > best;
         best = more ? vec[e].key[0] : best;
-        if constexpr (!packed) at = more ? vec[e].at((e * RT + lane) * VW) : at;
+        if constexpr (!packed) at = more ? vec[e].at(c[e]) : at;
       }
       const uint32_t m = group_umax<RT>(best);
       uint32_t j = 0;
@@ -266,7 +287,7 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
       for (int r = 0; r < KR; ++r)
         if (lane + r * RT == i) won[r] = m, won_at[r] = j;
 #pragma unroll
-      for (int e = 0; e < E; ++e) vec[e].pop(packed ? vec[e].key[0] == m : vec[e].at((e * RT + lane) * VW) == j);
+      for (int e = 0; e < E; ++e) vec[e].pop(packed ? vec[e].key[0] == m : vec[e].at(c[e]) == j);
     }
 #pragma unroll
     for (int r = 0; r < KR; ++r)

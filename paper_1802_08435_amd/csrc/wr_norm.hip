@@ -63,6 +63,33 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float* s) {
   }
 }
 
+// Columns of thread t's vector e: where it begins, how many of its first elements are not its own
+// (all VW past the row), and how many there are to load and store (0 past the row, the row's if it
+// is shorter than a vector).
+template <int RT, int VW>
+struct NormCols {
+  int c, skip, count;
+  __device__ __forceinline__ NormCols(int e, int t, int d) {
+    const int c0 = (e * RT + t) * VW;
+    c = d < VW ? 0 : vec_begin<VW>(c0, d);
+    skip = c0 >= d ? VW : c0 - c;
+    count = c0 >= d ? 0 : d < VW ? d : VW;
+  }
+  // A sum over the vector's own elements: add(k, s) is s with element k added.
+  template <class F>
+  __device__ __forceinline__ float sum(F add) const {
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < VW; ++k) s = add(k, s);
+    if (skip > 0 || count < VW) {   // (no lane of most waves)
+      s = 0.0f;
+#pragma unroll
+      for (int k = 0; k < VW; ++k) s = k >= skip && k < count ? add(k, s) : s;
+    }
+    return s;
+  }
+};
+
 template <class T, class W, int RT, int E>
 __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_kernel(NormArgs a) {
   constexpr int VW = 16 / sizeof(T), BT = RT < 256 ? 256 : RT, G = BT / RT;
@@ -72,9 +99,9 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_kernel(NormArgs a
   Raw<W, VW> ga[E], be[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const int c = (e * RT + t) * VW;
-    ga[e] = load_raw<W, VW>((const W*)a.gamma + c, a.gamma ? a.d - c : 0, (W)1.0f);
-    be[e] = load_raw<W, VW>((const W*)a.beta + c, a.beta ? a.d - c : 0);
+    const NormCols<RT, VW> q(e, t, a.d);
+    ga[e] = load_raw<W, VW>((const W*)a.gamma + q.c, a.gamma ? q.count : 0, (W)1.0f);
+    be[e] = load_raw<W, VW>((const W*)a.beta + q.c, a.beta ? q.count : 0);
   }
   for (int64_t i0 = (int64_t)blockIdx.x * G; i0 < a.n; i0 += (int64_t)gridDim.x * G) {
     const int64_t i = i0 + threadIdx.x / RT;
@@ -83,33 +110,37 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_kernel(NormArgs a
     T* y = (T*)a.y + i * a.y_stride;
     Raw<T, VW> raw[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) raw[e] = load_raw<T, VW>(x + (e * RT + t) * VW, on ? a.d - (e * RT + t) * VW : 0);
+    for (int e = 0; e < E; ++e) {
+      const NormCols<RT, VW> q(e, t, a.d);
+      raw[e] = load_raw<T, VW>(x + q.c, on ? q.count : 0);
+    }
     float v[E][VW], s[1] = {0.0f};
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int e = 0; e < E; ++e) {
+      const NormCols<RT, VW> q(e, t, a.d);
 #pragma unroll
-      for (int k = 0; k < VW; ++k) v[e][k] = (float)raw[e][k], s[0] += v[e][k];
+      for (int k = 0; k < VW; ++k) v[e][k] = (float)raw[e][k];
+      s[0] += q.sum([&](int k, float s) { return s + v[e][k]; });
+    }
     row_sums<RT, 1>(s, red[0]);
     const float m = s[0] * inv_d;
     s[0] = 0.0f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int c = (e * RT + t) * VW;
+      const NormCols<RT, VW> q(e, t, a.d);
 #pragma unroll
-      for (int k = 0; k < VW; ++k) {
-        v[e][k] -= m;
-        if (c + k < a.d) s[0] = __builtin_fmaf(v[e][k], v[e][k], s[0]);
-      }
+      for (int k = 0; k < VW; ++k) v[e][k] -= m;
+      s[0] += q.sum([&](int k, float s) { return __builtin_fmaf(v[e][k], v[e][k], s); });
     }
     row_sums<RT, 1>(s, red[1]);
     const float r = 1.0f / sqrtf(s[0] * inv_d + a.eps);
     if (on) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int c = (e * RT + t) * VW;
+        const NormCols<RT, VW> q(e, t, a.d);
 #pragma unroll
         for (int k = 0; k < VW; ++k) v[e][k] = __builtin_fmaf(v[e][k] * r, (float)ga[e][k], (float)be[e][k]);
-        store_part<T, VW>(y + c, v[e], a.d - c);
+        store_part<T, VW>(y + q.c, v[e], q.count);
       }
       if (t == 0) {
         if (a.mean) a.mean[i] = m;
@@ -187,8 +218,8 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_grad_kernel(NormG
   float dg[E][VW], db[E][VW];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const int c = (e * RT + t) * VW;
-    ga[e] = load_raw<W, VW>((const W*)a.gamma + c, a.gamma ? a.d - c : 0, (W)1.0f);
+    const NormCols<RT, VW> q(e, t, a.d);
+    ga[e] = load_raw<W, VW>((const W*)a.gamma + q.c, a.gamma ? q.count : 0, (W)1.0f);
 #pragma unroll
     for (int k = 0; k < VW; ++k) dg[e][k] = db[e][k] = 0.0f;
   }
@@ -199,35 +230,37 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_grad_kernel(NormG
     Raw<T, VW> rx[E], ry[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int c = (e * RT + t) * VW, count = on ? a.d - c : 0;
-      rx[e] = load_raw<T, VW>((const T*)a.x + i * a.x_stride + c, count);
-      ry[e] = load_raw<T, VW>((const T*)a.dy + i * a.dy_stride + c, count);   // (past the row 0: no part of any sum)
+      const NormCols<RT, VW> q(e, t, a.d);
+      rx[e] = load_raw<T, VW>((const T*)a.x + i * a.x_stride + q.c, on ? q.count : 0);
+      ry[e] = load_raw<T, VW>((const T*)a.dy + i * a.dy_stride + q.c, on ? q.count : 0);
     }
     const float m = on ? a.mean[i] : 0.0f, r = on ? a.rstd[i] : 0.0f;
     float h[E][VW], g[E][VW], s[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int e = 0; e < E; ++e) {
+      const NormCols<RT, VW> q(e, t, a.d);
 #pragma unroll
       for (int k = 0; k < VW; ++k) {
         h[e][k] = ((float)rx[e][k] - m) * r;
         g[e][k] = (float)ry[e][k];
-        if constexpr (WG) {
+        if constexpr (WG) {   // (each thread sums all its columns: a column of two threads comes out the same in both)
           dg[e][k] = __builtin_fmaf(g[e][k], h[e][k], dg[e][k]);
           db[e][k] += g[e][k];
         }
         g[e][k] *= (float)ga[e][k];
-        s[0] += g[e][k];
-        s[1] = __builtin_fmaf(g[e][k], h[e][k], s[1]);
       }
+      s[0] += q.sum([&](int k, float s) { return s + g[e][k]; });
+      s[1] += q.sum([&](int k, float s) { return __builtin_fmaf(g[e][k], h[e][k], s); });
+    }
     row_sums<RT, 2>(s, red[turn]);
     if (on && a.dx) {
       const float m0 = s[0] * inv_d, m1 = s[1] * inv_d;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int c = (e * RT + t) * VW;
+        const NormCols<RT, VW> q(e, t, a.d);
 #pragma unroll
         for (int k = 0; k < VW; ++k) g[e][k] = r * (g[e][k] - __builtin_fmaf(h[e][k], m1, m0));
-        store_part<T, VW>((T*)a.dx + i * a.dx_stride + c, g[e], a.d - c);
+        store_part<T, VW>((T*)a.dx + i * a.dx_stride + q.c, g[e], q.count);
       }
     }
   }
@@ -255,9 +288,9 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_grad_kernel(NormG
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int c = (e * RT + t) * VW;
-      store_part<float, VW>(p + c, dg[e], a.d - c);
-      store_part<float, VW>(p + a.d + c, db[e], a.d - c);
+      const NormCols<RT, VW> q(e, t, a.d);
+      store_part<float, VW>(p + q.c, dg[e], q.count);
+      store_part<float, VW>(p + a.d + q.c, db[e], q.count);
     }
   }
 }

@@ -79,6 +79,12 @@ __device__ __forceinline__ Raw<T, N> load_raw(const T* p, int count, T fill = (T
   }
   return x;
 }
+// Where a thread's vector at column c of a row of d elements begins: a row's last vector, if it is not
+// whole, is the last N elements, so that every load and store is of a whole vector.  Some columns are
+// then another thread's too: both come to the same values, and sums leave out the first
+// c - vec_begin of the vector (all of it past the row).  Only for d >= N.
+template <int N>
+__device__ __forceinline__ int vec_begin(int c, int d) { return c <= d - N ? c : d - N; }
 template <class T, int N>
 __device__ __forceinline__ void load_part(const T* p, float (&f)[N], int count) {
   const Raw<T, N> x = load_raw<T, N>(p, count);

@@ -265,7 +265,9 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_grad_kernel(NormG
     }
   }
   if constexpr (WG) {
-    float* p = a.part + (int64_t)blockIdx.x * 2 * a.d;
+    // (a single block's part is the whole)
+    float* pg = a.parts > 1 ? a.part + (int64_t)blockIdx.x * 2 * a.d : a.dgamma;
+    float* pb = a.parts > 1 ? pg + a.d : a.dbeta;
     if constexpr (G > 1) {   // the block's groups, in order
       __shared__ float sum[2][VW][BT];
 #pragma unroll
@@ -289,8 +291,8 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_grad_kernel(NormG
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const NormCols<RT, VW> q(e, t, a.d);
-      store_part<float, VW>(p + q.c, dg[e], q.count);
-      store_part<float, VW>(p + a.d + q.c, db[e], q.count);
+      store_part<float, VW>(pg + q.c, dg[e], pg ? q.count : 0);
+      store_part<float, VW>(pb + q.c, db[e], pb ? q.count : 0);
     }
   }
 }
@@ -348,9 +350,10 @@ __global__ __launch_bounds__(256) void wr_norm_wide_dw_kernel(NormGradArgs a) {
       db[k] += dy[k];
     }
   }
-  float* p = a.part + (int64_t)blockIdx.y * 2 * a.d;
-  store_part<float, 4>(p + c, dg, count);
-  store_part<float, 4>(p + a.d + c, db, count);
+  float* pg = a.parts > 1 ? a.part + (int64_t)blockIdx.y * 2 * a.d : a.dgamma;
+  float* pb = a.parts > 1 ? pg + a.d : a.dbeta;
+  store_part<float, 4>(pg + c, dg, pg ? count : 0);
+  store_part<float, 4>(pb + c, db, pb ? count : 0);
 }
 
 // The parts of 64 sums added: each of 16 waves every 16th part, then the waves in order.
@@ -442,7 +445,7 @@ wavernn_status run_norm_grad(NormGradArgs& a, void* stream) {
   } else {
     a.parts = 0;
   }
-  if (wg) WR_LAUNCH(wr_norm_parts_kernel, (2 * (int64_t)a.d + 63) / 64, 1024, 0, stream, a);
+  if (wg && a.parts != 1) WR_LAUNCH(wr_norm_parts_kernel, (2 * (int64_t)a.d + 63) / 64, 1024, 0, stream, a);
   return WAVERNN_OK;
 }
 
@@ -468,7 +471,8 @@ wavernn_status wavernn_layer_norm(int32_t dtype, const void* x_dev, int64_t n_ro
 
 int64_t wavernn_layer_norm_grad_workspace(int64_t n_rows, int32_t dim) {
   if (n_rows < 0 || n_rows > INT32_MAX || dim < 1 || dim > (1 << 30)) return -1;
-  return n_rows ? (int64_t)8 * dim * std::max(norm_parts(n_rows, dim, 2), norm_parts(n_rows, dim, 4)) : 0;
+  const int parts = std::max(norm_parts(n_rows, dim, 2), norm_parts(n_rows, dim, 4));
+  return n_rows > 0 && parts > 1 ? (int64_t)8 * dim * parts : 0;
 }
 
 wavernn_status wavernn_layer_norm_grad(int32_t dtype, const void* dy_dev, int64_t dy_stride, const void* x_dev,

@@ -17,7 +17,8 @@ import torch
 from . import wavernn as _w
 
 MAX_TOP = 32
-_raw_stream = torch._C._cuda_getCurrentRawStream    # (torch.cuda.current_stream() makes an object: 2.6 us)
+# (torch.cuda.current_stream() makes an object, which takes 2.6 us of a small call's 9)
+_raw_stream, _current_gpu = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 _DTYPE = {torch.float32: _w.F32, torch.bfloat16: _w.BF16, torch.float16: _w.F16}
 _ID_BYTES = {torch.int32: 4, torch.int64: 8}
 
@@ -30,13 +31,18 @@ def _dtype(name, t):
 
 def _rows(name, t):
     """(rows, elements of a row, elements from row to row) of t [..., width]."""
-    if t.dim() == 0:
+    shape = t.shape
+    if len(shape) == 2:
+        n, w = shape
+        step, one = t.stride()
+        if one != 1 and w > 1:
+            raise ValueError(f"{name}: the elements of a row must be adjacent")
+        return n, w, step if n > 1 else w
+    if not shape:
         raise ValueError(f"{name}: needs a last dimension of elements")
-    w = t.shape[-1]
+    w = shape[-1]
     if w > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: the elements of a row must be adjacent")
-    if t.dim() == 2:
-        return t.shape[0], w, t.stride(0)
     if t.dim() == 1:
         return 1, w, w
     n = 1
@@ -58,11 +64,10 @@ def _rows(name, t):
 
 def _plain(name, t, shape, dtypes, device):
     """t, checked to be contiguous, of the shape, on the device and of one of the dtypes."""
-    if t.shape != shape or t.device != device or t.dtype not in dtypes or not t.is_contiguous():
-        raise ValueError(f"{name}: needs a contiguous tensor {list(shape)} on {device}, "
-                         f"{' or '.join(str(d) for d in dtypes)}; got {t.dtype} {list(t.shape)} on {t.device}"
-                         f"{'' if t.is_contiguous() else ', not contiguous'}")
-    return t
+    if t.shape == shape and t.dtype in dtypes and t.device == device and t.is_contiguous():
+        return t
+    raise ValueError(f"{name}: needs a contiguous tensor {list(shape)} on {device}, {' or '.join(str(d) for d in dtypes)}; "
+                     f"got {t.dtype} {list(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
 
 
 def _result(name, out, shape, dtype, like):
@@ -83,19 +88,20 @@ def _p(t):
     return None if t is None else t.data_ptr()
 
 
-def _on_gpu(fn):
-    """Runs fn(t, ..., stream) with t's GPU current and, if a stream is given, that stream."""
-    def call(t, *args, stream=None, **kw):
-        if not t.is_cuda:
-            raise ValueError(f"{fn.__name__}: tensors must be on a GPU")
-        if stream is None and t.device.index == torch._C._cuda_getDevice():
-            return fn(t, *args, **kw)
-        if stream is not None and stream.device != t.device:
-            raise ValueError(f"{fn.__name__}: the stream is on {stream.device}, the tensors on {t.device}")
-        with torch.cuda.device(t.device), torch.cuda.stream(stream):
-            return fn(t, *args, **kw)
-    call.__name__, call.__doc__, call.__wrapped__ = fn.__name__, fn.__doc__, fn
-    return call
+def _away(t, stream):
+    """Is a call on t for another stream or GPU than the current ones?"""
+    gpu = t.device.index
+    return stream is not None or gpu is None or gpu != _current_gpu()
+
+
+def _there(fn, t, stream, *args):
+    """fn(*args) with t's GPU current and, if a stream is given, that stream."""
+    if not t.is_cuda:
+        raise ValueError(f"{fn.__name__}: tensors must be on a GPU")
+    if stream is not None and stream.device != t.device:
+        raise ValueError(f"{fn.__name__}: the stream is on {stream.device}, the tensors on {t.device}")
+    with torch.cuda.device(t.device), torch.cuda.stream(stream):
+        return fn(*args)
 
 
 _F32 = (torch.float32,)
@@ -103,15 +109,16 @@ _I32 = (torch.int32,)
 _IDS = (torch.int64, torch.int32)
 
 
-@_on_gpu
-def token_logprobs(logits, tokens=None, top=0):
+def token_logprobs(logits, tokens=None, top=0, stream=None):
     """Log probability of tokens [...] under logits [..., V], with the entropy, the log of the
     sum and the ``top`` most likely classes of every distribution: a dict of logp (None
     without tokens), entropy, lse [...], top_logp and top_idx [..., top] (None with top = 0), fp32 and
     int32.  tokens are int64 or int32; a negative one marks a row of padding, which is
     not read and gives 0 (top_idx -1).  Masked classes are -inf.  Edge cases and the order of
     alternatives: include/wavernn.h, wavernn_token_logprobs."""
-    L = _w.lib()
+    if _away(logits, stream):
+        return _there(token_logprobs, logits, stream, logits, tokens, top)
+    L = _w._lib or _w.lib()
     dt, (n, v, stride), dev, shape = _dtype("logits", logits), _rows("logits", logits), logits.device, logits.shape[:-1]
     if tokens is not None:
         _plain("tokens", tokens, shape, _IDS, dev)
@@ -133,14 +140,16 @@ def token_logprobs(logits, tokens=None, top=0):
     return dict(logp=logp, entropy=entropy, lse=lse, top_logp=top_logp, top_idx=top_idx)
 
 
-@_on_gpu
 def token_logprobs_grad(logits, tokens, lse, entropy=None, g_logp=None, g_entropy=None, g_lse=None, top_idx=None,
-                        g_top=None, out=None):
+                        g_top=None, out=None, stream=None):
     """Gradient with respect to the logits of a loss whose gradients with respect to
     token_logprobs' results are g_logp, g_entropy, g_lse [...] and g_top [..., top] (of top_logp; any
     may be None), given the results lse, entropy (for g_entropy) and top_idx (for g_top).
     ``out`` may be the logits themselves."""
-    L = _w.lib()
+    if _away(logits, stream):
+        return _there(token_logprobs_grad, logits, stream, logits, tokens, lse, entropy, g_logp, g_entropy, g_lse, top_idx,
+                      g_top, out)
+    L = _w._lib or _w.lib()
     dt, (n, v, stride), dev, shape = _dtype("logits", logits), _rows("logits", logits), logits.device, logits.shape[:-1]
     if tokens is not None:
         _plain("tokens", tokens, shape, _IDS, dev)
@@ -170,12 +179,13 @@ def _table_dtype(name, dtype, like):
     return dtype
 
 
-@_on_gpu
-def embed(table, ids, scale=1.0, dtype=None, out=None):
+def embed(table, ids, scale=1.0, dtype=None, out=None, stream=None):
     """scale * table[ids]: rows of table [V, d] for ids [...] (int64 or int32) as [..., d], of the
     table's dtype or float32.  A negative id is padding (zeros); one of V or more gives NaN.
     ``out`` [..., d] may be a slice of wider rows."""
-    L = _w.lib()
+    if _away(table, stream):
+        return _there(embed, table, stream, table, ids, scale, dtype, out)
+    L = _w._lib or _w.lib()
     dt, dev = _dtype("table", table), table.device
     if table.dim() != 2:
         raise ValueError("table: needs two dimensions")
@@ -188,12 +198,13 @@ def embed(table, ids, scale=1.0, dtype=None, out=None):
     return out
 
 
-@_on_gpu
-def embed_grad(dout, ids, n_rows, scale=1.0, dtype=torch.float32):
+def embed_grad(dout, ids, n_rows, scale=1.0, dtype=torch.float32, stream=None):
     """Gradient of embed's table [n_rows, d] from dout [..., d] and ids [...]: scale times
     the sum of dout's rows for each number, zero for numbers that do not occur; sums in fp32 in an
     order of their own, the same every time.  dtype: float32 or dout's."""
-    L = _w.lib()
+    if _away(dout, stream):
+        return _there(embed_grad, dout, stream, dout, ids, n_rows, scale, dtype)
+    L = _w._lib or _w.lib()
     dt, (n, d, stride), dev = _dtype("dout", dout), _rows("dout", dout), dout.device
     _plain("ids", ids, dout.shape[:-1], _IDS, dev)
     dtype = _table_dtype("embed_grad", dtype, dout.dtype)
@@ -213,12 +224,13 @@ def _weight(name, w, d, t, other=None):
         raise ValueError("gamma and beta must be of one dtype")
 
 
-@_on_gpu
-def layer_norm(x, gamma=None, beta=None, eps=1e-5, stats=False, out=None):
+def layer_norm(x, gamma=None, beta=None, eps=1e-5, stats=False, out=None, stream=None):
     """(x - mean) / sqrt(variance + eps) * gamma + beta over the last dimension of x [..., d], of x's
     dtype; gamma, beta [d] of x's dtype or float32.  With ``stats`` also the rows' mean and
     1 / sqrt(variance + eps) [...], which layer_norm_grad takes.  ``out`` may be x."""
-    L = _w.lib()
+    if _away(x, stream):
+        return _there(layer_norm, x, stream, x, gamma, beta, eps, stats, out)
+    L = _w._lib or _w.lib()
     dt, (n, d, stride), dev = _dtype("x", x), _rows("x", x), x.device
     _weight("gamma", gamma, d, x)
     _weight("beta", beta, d, x, gamma)
@@ -232,12 +244,13 @@ def layer_norm(x, gamma=None, beta=None, eps=1e-5, stats=False, out=None):
     return (y, mean, rstd) if stats else y
 
 
-@_on_gpu
-def layer_norm_grad(dy, x, mean, rstd, gamma=None, weights=True, out=None):
+def layer_norm_grad(dy, x, mean, rstd, gamma=None, weights=True, out=None, stream=None):
     """(dx, dgamma, dbeta) of layer_norm from dy [..., d], its x and the statistics it
     returned; dx of x's dtype, dgamma and dbeta [d] float32 (None without ``weights``).  ``out``
     (for dx) may be dy or x."""
-    L = _w.lib()
+    if _away(x, stream):
+        return _there(layer_norm_grad, x, stream, dy, x, mean, rstd, gamma, weights, out)
+    L = _w._lib or _w.lib()
     dt, (n, d, stride), dev = _dtype("x", x), _rows("x", x), x.device
     if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != dev:
         raise ValueError("dy must be of x's shape, dtype and device")

@@ -134,6 +134,7 @@ def test_row_views():
     assert ops._rows("t", torch.zeros(1, 5).expand(7, 5)) == (7, 5, 0)
     assert ops._rows("t", torch.zeros(1, 1, 5).expand(7, 3, 5)) == (21, 5, 0)
     assert ops._rows("t", torch.zeros(0, 3, 5)) == (0, 5, 5)
+    assert ops._rows("t", torch.zeros(1, 5).as_strided((1, 5), (1 << 33, 1))) == (1, 5, 5)   # (no second row)
     assert ops._rows("t", torch.zeros(4, 1)[:, :1]) == (4, 1, 1)
     for bad in (t[..., ::2], t.transpose(1, 2), t[:, :4, :], torch.zeros(())):
         with pytest.raises(ValueError):

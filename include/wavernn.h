@@ -344,7 +344,7 @@ wavernn_status wavernn_token_logprobs(int32_t dtype, const void* logits_dev, int
  *   dlogits_j = [j = token] g_logp + sum_k [j = top_idx_k] g_top_k
  *               + p_j (g_lse - g_logp - sum_k g_top_k) - g_entropy p_j (log p_j + entropy),
  * p_j = exp(z_j - lse), from the forward call's lse, entropy (needed with
- * g_entropy) and top_idx (needed with top > 0; a negative one, and its g_top, is
+ * g_entropy) and top_idx (needed with top > 0; one that is no class, and its g_top, is
  * ignored).  Rows of padding and rows whose every class is masked are zero whatever
  * the gradients hold there; with g_logp a token of n_classes or more makes its row NaN.  dlogits
  * is of the logits' type and may be the logits (same stride). */

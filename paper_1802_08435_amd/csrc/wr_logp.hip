@@ -15,6 +15,7 @@
 
 #define LOGP_BLOCKS 2048   // eight blocks of 256 threads a CU
 #define LW_SPLITS 128      // most segments of a row
+#define LW_SEG 8192        // fewest classes of one (but for rounding)
 
 namespace {
 
@@ -544,24 +545,23 @@ __global__ __launch_bounds__(256) void wr_logp_join_kernel(LogpArgs a) {
       q = soft_join(q, Soft{__shfl_xor(q.m, d, 64), __shfl_xor(q.s, d, 64), __shfl_xor(q.w, d, 64)});
     if (tid == 0) put_row(a, o, t, (const T*)a.logits + row * a.stride, q, soft_sub(q));
     if (a.top == 0) continue;
-    // The segments' best classes come first: the top-th largest of them is a lower bound, reached in at
-    // most `top` segments, so at most top^2 classes are ranked.
+    // Each segment's classes come in order, so the top-th largest of their first few (enough that there are
+    // `top` of them) is a lower bound, and what reaches it is ranked: with a bound from the best ones alone
+    // it is reached in at most `top` segments, at most top^2 classes.
     const u64* keys = a.part_keys + row * a.splits * a.top;
-    if (tid < a.splits) sh.list[tid] = keys[tid * a.top];
+    const int first = (a.top + a.splits - 1) / a.splits, heads = first * a.splits;   // heads < 2 top or = splits
+    if (tid < heads) sh.list[tid] = keys[tid / first * a.top + tid % first];
     if (tid == 0) sh.count = 0;
-    u64 low = 0;
     __syncthreads();
-    if (a.splits >= a.top) {
-      if (tid < a.splits) {
-        const u64 mine = sh.list[tid];
-        int r = 0;
+    if (tid < heads) {
+      const u64 mine = sh.list[tid];
+      int r = 0;
 #pragma unroll 8
-        for (int j = 0; j < a.splits; ++j) r += sh.list[j] > mine;
-        if (r == a.top - 1) sh.wave_best[0] = mine;
-      }
-      __syncthreads();
-      low = sh.wave_best[0];
+      for (int j = 0; j < heads; ++j) r += sh.list[j] > mine;
+      if (r == a.top - 1) sh.wave_best[0] = mine;
     }
+    __syncthreads();
+    const u64 low = sh.wave_best[0];
     __syncthreads();
     for (int i = tid; i < a.splits * a.top; i += 256) {
       const u64 key = keys[i];
@@ -608,7 +608,7 @@ __global__ __launch_bounds__(256) void wr_logp_grad_kernel(LogpGradArgs a) {
     const float* tg = a.g_top + row * a.f.top;
     if (!zero)
       for (int k = 0; k < a.f.top; ++k)
-        if (ti[k] >= 0) gp -= tg[k];
+        if (ti[k] >= 0 && ti[k] < v) gp -= tg[k];
 #pragma unroll
     for (int u = 0; u < LG_U; ++u) {
       const int64_t j = i0 + (int64_t)u * rt * VW;
@@ -653,10 +653,10 @@ wavernn_status check_tokens(const void* tokens, int bytes, int* kind) {
 }  // namespace
 
 // Segments of a row: one, unless there are too few rows for the card (a row each for fewer than 512
-// blocks, two a CU) and they are long: then as many as give 1,024 blocks, of 4,096 classes at least.
+// blocks, two a CU) and they are long: then as many as give 1,024 blocks, of LW_SEG classes at least.
 static int logp_splits(int64_t n, int32_t v) {
   if (n < 1 || n >= 512) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({LW_SPLITS, 1024 / n, ((int64_t)v + 4095) / 4096}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({LW_SPLITS, 1024 / n, ((int64_t)v + LW_SEG - 1) / LW_SEG}));
 }
 
 template <class T>

@@ -272,6 +272,15 @@ def test_logprobs_gradient(n, v, dt):
                            dz.nan_to_num(7.0)), "in place"
 
 
+def test_logprobs_gradient_ignores_alternatives_that_are_no_class():
+    z, t = randn(5, 50, seed=2), tokens_for(5, 50)
+    r = ops.token_logprobs(z, t, top=2)
+    g = randn(5, 4, seed=3)
+    idx = torch.cat([r["top_idx"], torch.tensor([[-1, 50]] * 5, dtype=torch.int32, device="cuda")], 1)
+    a = ops.token_logprobs_grad(z, t, r["lse"], top_idx=idx, g_top=g)
+    assert torch.equal(a, ops.token_logprobs_grad(z, t, r["lse"], top_idx=r["top_idx"], g_top=g[:, :2].contiguous()))
+
+
 def test_logprobs_gradient_special_rows():
     z = randn(5, 300, seed=3)
     z[1] = -INF                      # nothing left

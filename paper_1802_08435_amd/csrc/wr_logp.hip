@@ -219,7 +219,7 @@ struct TopVec<float> {   // sorted by neighbours' exchanges, which keep equal lo
 // Each vector is sorted for itself; then the alternatives are drawn one by one, each
 // lane offering its best class left.  With 16 lanes a row four rows share every
 // reduction of a wave.
-template <class T, int RT, int E>
+template <class T, int RT, int E, bool TAIL>
 __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
   constexpr int VW = 16 / sizeof(T), KR = (WAVERNN_MAX_TOP + RT - 1) / RT;
   constexpr bool packed = sizeof(T) == 2;
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int c0 = (e * RT + lane) * VW;
-      c[e] = a.v < VW || c0 >= a.v ? c0 : vec_begin<VW>(c0, a.v);
+      c[e] = !TAIL || a.v < VW || c0 >= a.v ? c0 : vec_begin<VW>(c0, a.v);
       raw[e] = load_raw<T, VW>(zr + c[e], a.v - c[e], (T)-__builtin_inff());
     }
     float z[E][VW];
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
     for (int e = 0; e < E; ++e) {
 #pragma unroll
       for (int k = 0; k < VW; ++k) z[e][k] = (float)raw[e][k];
-      if (c[e] < (e * RT + lane) * VW)   // (no lane of most waves)
+      if (TAIL && c[e] < (e * RT + lane) * VW)   // (no lane of most waves)
 #pragma unroll
         for (int k = 0; k < VW; ++k)
           if (c[e] + k < (e * RT + lane) * VW) z[e][k] = -__builtin_inff();
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
       if (q.s != q.s)
 #pragma unroll
         for (int k = 0; k < VW; ++k) z[e][k] = plain_nan(z[e][k]);
-      vec[e].init(z[e], c[e], (e * RT + lane) * VW);
+      vec[e].init(z[e], c[e], TAIL ? (e * RT + lane) * VW : c[e]);
     }
     uint32_t won[KR] = {}, won_at[KR] = {};
     for (int i = 0; i < a.top; ++i) {
@@ -659,24 +659,27 @@ static int logp_splits(int64_t n, int32_t v) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({LW_SPLITS, 1024 / n, ((int64_t)v + LW_SEG - 1) / LW_SEG}));
 }
 
+template <class T, bool TAIL>
+static wavernn_status rows_launch(LogpArgs& a, int vecs, void* stream) {
+  auto blocks = [&](int rows) { return std::min<int64_t>((a.n + rows - 1) / rows, LOGP_BLOCKS); };
+  if (vecs <= 16) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 1, TAIL>), blocks(16), 256, 0, stream, a);
+  else if (vecs <= 32) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 2, TAIL>), blocks(16), 256, 0, stream, a);
+  else if (vecs <= 64) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 4, TAIL>), blocks(16), 256, 0, stream, a);
+  else if (vecs <= 128) WR_LAUNCH((wr_logp_rows_kernel<T, 32, 4, TAIL>), blocks(8), 256, 0, stream, a);
+  else if (vecs <= 256) WR_LAUNCH((wr_logp_rows_kernel<T, 64, 4, TAIL>), blocks(4), 256, 0, stream, a);
+  else WR_LAUNCH((wr_logp_rows_kernel<T, 64, 8, TAIL>), blocks(4), 256, 0, stream, a);
+  return WAVERNN_OK;
+}
 template <class T>
 static wavernn_status logp_launch(LogpArgs& a, void* stream) {
   constexpr int VW = 16 / sizeof(T);
   const int vecs = (int)(((int64_t)a.v + VW - 1) / VW);
-  auto blocks = [&](int rows) { return std::min<int64_t>((a.n + rows - 1) / rows, LOGP_BLOCKS); };
-  if (vecs <= 16) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 1>), blocks(16), 256, 0, stream, a);
-  else if (vecs <= 32) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 2>), blocks(16), 256, 0, stream, a);
-  else if (vecs <= 64) WR_LAUNCH((wr_logp_rows_kernel<T, 16, 4>), blocks(16), 256, 0, stream, a);
-  else if (vecs <= 128) WR_LAUNCH((wr_logp_rows_kernel<T, 32, 4>), blocks(8), 256, 0, stream, a);
-  else if (vecs <= 256) WR_LAUNCH((wr_logp_rows_kernel<T, 64, 4>), blocks(4), 256, 0, stream, a);
-  else if (vecs <= 512) WR_LAUNCH((wr_logp_rows_kernel<T, 64, 8>), blocks(4), 256, 0, stream, a);
-  else {
-    a.splits = a.part ? logp_splits(a.n, a.v) : 1;
-    a.seg = (int)(((int64_t)a.v + a.splits - 1) / a.splits + 7) / 8 * 8;
-    a.part_keys = (u64*)((LogpPart*)a.part + a.n * a.splits);
-    WR_LAUNCH((wr_logp_kernel<T>), std::min<int64_t>(a.n * a.splits, LOGP_BLOCKS), 256, 0, stream, a);
-    if (a.splits > 1) WR_LAUNCH((wr_logp_join_kernel<T>), a.n, 256, 0, stream, a);
-  }
+  if (vecs <= 512) return a.v % VW ? rows_launch<T, true>(a, vecs, stream) : rows_launch<T, false>(a, vecs, stream);
+  a.splits = a.part ? logp_splits(a.n, a.v) : 1;
+  a.seg = (int)(((int64_t)a.v + a.splits - 1) / a.splits + 7) / 8 * 8;
+  a.part_keys = (u64*)((LogpPart*)a.part + a.n * a.splits);
+  WR_LAUNCH((wr_logp_kernel<T>), std::min<int64_t>(a.n * a.splits, LOGP_BLOCKS), 256, 0, stream, a);
+  if (a.splits > 1) WR_LAUNCH((wr_logp_join_kernel<T>), a.n, 256, 0, stream, a);
   return WAVERNN_OK;
 }
 wavernn_status wr_logp_launch(int dtype, LogpArgs& a, void* stream) {

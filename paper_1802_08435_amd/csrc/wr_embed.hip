@@ -426,10 +426,11 @@ __global__ __launch_bounds__(256) void wr_embed_join_kernel(EmbedGradArgs a) {
 }
 
 // ---- few rows ----------------------------------------------------------------
-// A table of up to EF_ROWS rows (bytes, labels): block (v, s) looks for number v among the ids of segment s
+// A table of up to EF_ROWS rows (bytes, labels), with up to EF_WORK ids compared: block (v, s) looks for number v among the ids of segment s
 // itself, which takes no sort, and sums the rows it finds; with several segments one more launch adds
 // their sums in order.  12,800 rows of 64 into 97: 22 us by the sort (four launches), EF_TIME.
 #define EF_ROWS 256
+#define EF_WORK (4 << 20)  // ids times rows
 #define EF_SEG 2048        // ids of a segment: 8 a thread; more (up to 8,192) past 64 segments
 #define EF_SEG_MAX 8192
 #define EF_SEGS 64
@@ -519,7 +520,7 @@ __global__ __launch_bounds__(256) void wr_embed_few_join_kernel(EmbedGradArgs a)
 
 // Sizes of a call and its workspace's layout; returns the workspace's bytes.
 int64_t plan_embed_grad(int64_t n, int32_t dim, int64_t v, EmbedGradArgs* a, unsigned char* ws) {
-  a->few = v <= EF_ROWS && n <= (int64_t)EF_SEGS * EF_SEG_MAX;
+  a->few = v <= EF_ROWS && n * v <= EF_WORK && n <= (int64_t)EF_SEGS * EF_SEG_MAX;
   if (a->few) {
     a->tile = EF_SEG;
     while (n > (int64_t)EF_SEGS * a->tile) a->tile *= 2;
@@ -559,7 +560,8 @@ template <class T, class U>
 wavernn_status run_embed_grad(EmbedGradArgs& a, void* stream) {
   if (a.few) {
     constexpr int VW = vec_of<T, U>();
-    a.row_threads = wr_row_threads(((int64_t)a.dim + VW - 1) / VW);
+    // (16 threads a row at least: a block finds few rows, and its groups are added one by one)
+    a.row_threads = std::max(16, wr_row_threads(((int64_t)a.dim + VW - 1) / VW));
     void* argv[] = {&a};
     const hipError_t e = hipLaunchKernel((const void*)wr_embed_few_kernel<T, U>, dim3(a.v, a.tiles), dim3(256), argv, 0,
                                          (hipStream_t)stream);

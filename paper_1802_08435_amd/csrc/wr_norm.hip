@@ -25,7 +25,7 @@ constexpr NormShape kShapes[] = {{16, 16, 1},  {64, 64, 1},    {128, 64, 2},   {
                                  {512, 256, 2}, {1024, 256, 4}, {2048, 512, 4}, {4096, 1024, 4}};
 
 #define NORM_BLOCKS 2048       // forward: eight blocks of 256 threads a CU
-#define NORM_GRAD_BLOCKS 512   // backward: parts of dgamma and dbeta
+#define NORM_GRAD_BT 512       // backward: threads of a block, where a row takes fewer
 
 struct NormArgs {
   const void* x;
@@ -44,7 +44,7 @@ __device__ __forceinline__ float group_sum(float v) {
   for (int o = (RT < 64 ? RT : 64) / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
 }
-// Sums of K values over the RT threads of a row; `s` (RT > 64): [waves][K], another one for the next sum.
+// Sums of K values over the RT threads of a row; `s` (RT > 64): [waves of the block][K], another one for the next sum.
 template <int RT, int K>
 __device__ __forceinline__ void row_sums(float (&v)[K], float* s) {
 #pragma unroll
@@ -54,6 +54,7 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float* s) {
 #pragma unroll
       for (int k = 0; k < K; ++k) s[(threadIdx.x >> 6) * K + k] = v[k];
     __syncthreads();
+    s += threadIdx.x / RT * (RT / 64) * K;   // this row's waves
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       v[k] = s[k];
@@ -209,8 +210,8 @@ struct NormGradArgs {
 
 // dx, and with WG this block's part of dgamma and dbeta.
 template <class T, class W, int RT, int E, bool WG>
-__global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_grad_kernel(NormGradArgs a) {
-  constexpr int VW = 16 / sizeof(T), BT = RT < 256 ? 256 : RT, G = BT / RT;
+__global__ __launch_bounds__(RT < NORM_GRAD_BT ? NORM_GRAD_BT : RT) void wr_norm_grad_kernel(NormGradArgs a) {
+  constexpr int VW = 16 / sizeof(T), BT = RT < NORM_GRAD_BT ? NORM_GRAD_BT : RT, G = BT / RT;
   __shared__ float red[2][BT / 64 * 2];
   const int t = threadIdx.x % RT;
   const float inv_d = 1.0f / (float)a.d;
@@ -414,13 +415,14 @@ wavernn_status run_norm(NormArgs& a, void* stream) {
   return WAVERNN_OK;
 }
 
-// Parts of dgamma and dbeta of a call (dtype's bytes matter to the shape): two
-// rows for each group of threads at least, so that the parts stay smaller than the rows.
+// Parts of dgamma and dbeta of a call (dtype's bytes matter to the shape), a block each: one a CU where a
+// thread keeps 16 columns, two where fewer (20,000 x 257 fp32, 8 columns: 16.7 us with 512 parts, 20.0 with 256;
+// 20,000 x 768 bf16, 16 columns: 27.7 and 24.9, the parts being large), and two rows for each group of threads at least.
 int norm_parts(int64_t n, int32_t d, int bytes) {
   const int i = norm_shape(((int64_t)d * bytes + 15) / 16);
-  const int rt = i < (int)(sizeof kShapes / sizeof kShapes[0]) ? kShapes[i].rt : 256;
-  const int g = rt < 256 ? 256 / rt : 1;
-  return (int)std::min<int64_t>(NORM_GRAD_BLOCKS, std::max<int64_t>(1, (n + 2 * g - 1) / (2 * g)));
+  const bool wide = i >= (int)(sizeof kShapes / sizeof kShapes[0]);
+  const int rt = wide ? NORM_GRAD_BT : kShapes[i].rt, g = rt < NORM_GRAD_BT ? NORM_GRAD_BT / rt : 1;
+  return (int)std::min<int64_t>(!wide && kShapes[i].e * 16 / bytes >= 16 ? 256 : 512, std::max<int64_t>(1, (n + 2 * g - 1) / (2 * g)));
 }
 
 template <class T, class W>
@@ -438,7 +440,7 @@ wavernn_status run_norm_grad(NormGradArgs& a, void* stream) {
                  if (e != hipSuccess) return wr_fail(WAVERNN_E_HIP, "launch of wr_norm_wide_dw_kernel: %s", hipGetErrorString(e));
                }
                if (a.dx) WR_LAUNCH((wr_norm_grad_wide_kernel<T, W>), std::min<int64_t>(a.n, NORM_BLOCKS), 1024, 0, stream, a),
-               constexpr int BT = RT < 256 ? 256 : RT;
+               constexpr int BT = RT < NORM_GRAD_BT ? NORM_GRAD_BT : RT;
                if (wg) WR_LAUNCH((wr_norm_grad_kernel<T, W, RT, E, true>), a.parts, BT, 0, stream, a);
                else WR_LAUNCH((wr_norm_grad_kernel<T, W, RT, E, false>),
                               std::min<int64_t>((a.n + BT / RT - 1) / (BT / RT), NORM_BLOCKS), BT, 0, stream, a));

@@ -375,7 +375,8 @@ wavernn_status wavernn_embed_grad(int32_t dout_dtype, const void* dout_dev, int6
 /* Layer norm of rows of `dim` elements: y = (x - mean) rstd gamma + beta with the
  * row's mean and rstd = 1 / sqrt(variance + eps), eps > 0.  gamma, beta [dim] are of
  * w_dtype (x's type or F32), NULL = 1 and 0.  mean, rstd [n_rows] (NULL: not
- * wanted) are what the gradient needs.  y may be x (same stride). */
+ * wanted) are what the gradient needs.  y may be x (same stride).  Elements past about 1e18 overflow
+ * the fp32 variance. */
 wavernn_status wavernn_layer_norm(int32_t dtype, const void* x_dev, int64_t n_rows, int32_t dim, int64_t x_stride,
                                   int32_t w_dtype, const void* gamma_dev, const void* beta_dev, float eps, void* y_dev,
                                   int64_t y_stride, float* mean_dev, float* rstd_dev, void* stream);

@@ -418,6 +418,24 @@ def test_embed_gradient_many_tokens(n, v, d, kind):
     check_embed_grad(dout, ids, v, 1.0, F32)
 
 
+@pytest.mark.parametrize("n,v,d,kind", [(70001, 3000, 1024, "skew"), (2200000, 1000, 8, "skew"), (700001, 400, 4, "sorted"),
+                                        (5000, (1 << 27) + 5, 1, "even")])
+def test_embed_gradient_largest(n, v, d, kind):
+    """Long chunks, sort tiles of several pieces, numbers of 28 bits."""
+    check_embed_grad(randn(n, d, seed=2, dt=BF16), ids_for(kind, n, v), v, 1.0, F32)
+
+
+def test_embed_far_rows():
+    """Table and result rows past 2^31 elements."""
+    step = 2 ** 30 + 7
+    store = torch.zeros(2 * step + 64, dtype=BF16, device="cuda")
+    table = store.as_strided((3, 40), (step, 1))
+    table.copy_(randn(3, 40, seed=6, dt=BF16))
+    ids = torch.tensor([2, 1, 0], device="cuda")
+    out = torch.zeros_like(store).as_strided((3, 40), (step, 1))
+    assert torch.equal(ops.embed(table, ids, scale=2.0, out=out), 2.0 * table[ids])
+
+
 def test_embed_gradient_views_and_no_tokens():
     wide = randn(6, 50, 100, seed=2)
     ids = tokens_for(300, 20).reshape(6, 50)
@@ -538,6 +556,19 @@ def test_layer_norm_views_and_edges():
     x[1, 5] = NAN
     y = ops.layer_norm(x)
     assert torch.isnan(y[1]).all() and torch.isfinite(y[0]).all() and torch.isfinite(y[2]).all()
+
+
+def test_layer_norm_far_rows():
+    """Row offsets past 2^31 elements."""
+    step = 2 ** 30 + 9
+    store = torch.zeros(2 * step + 128, dtype=BF16, device="cuda")
+    x = store.as_strided((3, 100), (step, 1))
+    x.copy_(randn(3, 100, seed=7, dt=BF16))
+    y, mean, rstd = ops.layer_norm(x, stats=True)
+    near = x.contiguous()
+    assert torch.equal(y, ops.layer_norm(near))
+    far = ops.layer_norm_grad(x, x, mean, rstd)
+    assert all(torch.equal(a, b) for a, b in zip(far, ops.layer_norm_grad(near, near, mean, rstd)))
 
 
 def test_layer_norm_large_mean():

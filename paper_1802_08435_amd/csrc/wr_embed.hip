@@ -62,8 +62,9 @@ __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
 // 262,143 rows, 1 to 511).  A wave ranks 64 numbers at a time: the lanes that
 // hold the same digit find each other by ballots, and the wave's count of that
 // digit, in LDS, is the base of their ranks.  Up to 4,096 ids one block does all
-// passes in LDS; more take two launches a pass (digit counts of every tile, then the
-// scatter), tiles of SORT_TILE ids, at most 256 tiles.
+// passes in LDS; more take tiles of SORT_TILE ids, at most 256 tiles, and two launches a
+// pass (digit counts of every tile, then the scatter), or one where each tile's block can count
+// all ids itself (up to SORT_SELF tiles).
 //
 // The sort leaves the memory idle, so further blocks of its launches clear the table
 // meanwhile, all of it: which rows stay without a number is not known yet.
@@ -80,6 +81,7 @@ __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
 #define SORT_SMALL 4096
 #define SORT_TILE 2048
 #define SORT_TILES 256
+#define SORT_SELF 8        // (16,384 rows of 1,024 into 50,000: 68 us with counts, 63 so; 32,768: 36 and, so, 48)
 #define EG_AHEAD 8
 #define EG_CHUNK_MIN 8      // positions of a chunk: doubled up to 64 while that leaves 1,024 blocks, four a CU (and 64 KiB of LDS are enough)
 #define EG_CHUNK_MAX 64
@@ -271,7 +273,27 @@ __global__ __launch_bounds__(SORT_THREADS) void wr_sort_scatter_kernel(EmbedGrad
     }
   };
   read((int64_t)blockIdx.x * a.tile);
-  {   // this tile's first place of each digit: all smaller digits, and this one in the tiles before
+  // this tile's first place of each digit: all smaller digits, and this one in the tiles before
+  if (a.tiles <= SORT_SELF) {
+    for (int i = tid; i < 4 * SORT_BINS; i += SORT_THREADS) (i < 2 * SORT_BINS ? before[0] : total[0])[i % (2 * SORT_BINS)] = 0;
+    __syncthreads();
+    const int first = (int)blockIdx.x * a.tile;
+    for (int i0 = tid; i0 < a.n; i0 += SORT_THREADS * 4) {
+      uint32_t x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * SORT_THREADS;
+        x[u] = i < a.n ? (a.src < 0 ? sort_key(a, i) : a.key[a.src][i]) : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * SORT_THREADS;
+        if (i < a.n) atomicAdd(i < first ? &before[0][(x[u] >> a.shift) & mask] : &total[0][(x[u] >> a.shift) & mask], 1u);
+      }
+    }
+    __syncthreads();
+    if (tid < SORT_BINS) total[0][tid] += before[0][tid];
+  } else {
     const int d = tid & (SORT_BINS - 1), half = tid / SORT_BINS;
     uint32_t b = 0, t = 0;
 #pragma unroll 8
@@ -428,7 +450,8 @@ __global__ __launch_bounds__(256) void wr_embed_join_kernel(EmbedGradArgs a) {
 // ---- few rows ----------------------------------------------------------------
 // A table of up to EF_ROWS rows (bytes, labels), with up to EF_WORK ids compared: block (v, s) looks for number v among the ids of segment s
 // itself, which takes no sort, and sums the rows it finds; with several segments one more launch adds
-// their sums in order.  12,800 rows of 64 into 97: 22 us by the sort (four launches), EF_TIME.
+// their sums in order.  12,800 rows of 64 into 97: 20 us by the
+// sort (four launches), 12 so; 100,000 rows of 16 into 256, past EF_WORK: 74 so, 33 by the sort.
 #define EF_ROWS 256
 #define EF_WORK (4 << 20)  // ids times rows
 #define EF_SEG 2048        // ids of a segment: 8 a thread; more (up to 8,192) past 64 segments
@@ -572,7 +595,8 @@ wavernn_status run_embed_grad(EmbedGradArgs& a, void* stream) {
   }
   int last = 0;
   const bool small = a.n <= SORT_SMALL;
-  const int launches = small ? 1 : 2 * a.passes;
+  const bool counts = a.tiles > SORT_SELF;
+  const int launches = small ? 1 : counts ? 2 * a.passes : a.passes;
   const int64_t bytes = (int64_t)a.v * a.dim * sizeof(U);
   auto clear = [&](int i) {   // launch i's share of the table, in 16-byte pieces; its blocks
     a.clear0 = bytes / 16 * i / launches * 16;
@@ -590,8 +614,8 @@ wavernn_status run_embed_grad(EmbedGradArgs& a, void* stream) {
     for (int pass = 0; pass < a.passes; ++pass) {
       a.src = pass == 0 ? -1 : (pass - 1) & 1;
       a.shift = pass * a.bits;
-      WR_LAUNCH(wr_sort_count_kernel, clear(2 * pass), SORT_THREADS, 0, stream, a);
-      WR_LAUNCH(wr_sort_scatter_kernel, clear(2 * pass + 1), SORT_THREADS, 0, stream, a);
+      if (counts) WR_LAUNCH(wr_sort_count_kernel, clear(2 * pass), SORT_THREADS, 0, stream, a);
+      WR_LAUNCH(wr_sort_scatter_kernel, clear(counts ? 2 * pass + 1 : pass), SORT_THREADS, 0, stream, a);
     }
     last = (a.passes - 1) & 1;
   }

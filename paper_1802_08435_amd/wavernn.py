@@ -208,8 +208,7 @@ class Model:
         """Rows [S][n_frames][cond_dim] before the layer norm, of labels or as given."""
         from . import ops
         if x.dtype.is_floating_point:
-            if x.dim() != 3 or x.shape[2] != self.cond_dim:
-                raise ValueError(f"features must be [S][n_frames][{self.cond_dim}], got {list(x.shape)}")
+            self._check_frames("features", x)
             return x
         if self.E is None:
             raise ValueError("labels need a model with a label table (E)")
@@ -220,6 +219,11 @@ class Model:
         if x.dim() != 3 or x.shape[2] != fields:
             raise ValueError(f"labels must be [S][n_frames][{fields}], got {list(x.shape)}")
         return ops.embed(self.E, x, scale=self.E_scale, stream=stream).view(x.shape[0], x.shape[1], self.cond_dim)
+
+    def _check_frames(self, name, x):
+        import torch
+        if x.dim() != 3 or x.shape[2] != self.cond_dim or x.dtype != torch.float32 or not x.is_contiguous():
+            raise ValueError(f"{name} must be contiguous float32 [S][n_frames][{self.cond_dim}], got {x.dtype} {list(x.shape)}")
 
     def frames(self, x, stream=None):
         """Conditioning frames [S][n_frames][cond_dim] fp32, as sample and score take them, through the
@@ -236,6 +240,9 @@ class Model:
         frames(x): a dict of E, ln_g, ln_b (None where the model has none or x are features)
         and x (with respect to features; None for labels)."""
         from . import ops
+        self._check_frames("dframes", dframes)
+        if dframes.shape[:2] != x.shape[:2]:
+            raise ValueError(f"dframes {list(dframes.shape)} and x {list(x.shape)} must have the same frames")
         labels = None if x.dtype.is_floating_point else x
         grads = dict(E=None, ln_g=None, ln_b=None, x=None)
         d = dframes

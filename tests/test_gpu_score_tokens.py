@@ -147,6 +147,13 @@ def test_front_end_gradient_against_differences():
         assert abs(float(num) - ana) <= float(df.abs().sum()) * (1000 * step * step / 6 + 1e-5)
     x = torch.randn(2, 7, 16, device="cuda", generator=g)
     by = m.frames_grad(x, df[:2, :7].contiguous())
+    with pytest.raises(ValueError, match="float32"):
+        m.frames(x.bfloat16())
+    with pytest.raises(ValueError, match="contiguous"):
+        m.frames(x.expand(2, 7, 16).transpose(0, 1))
+    for bad in (df[:, :39], df[:, :, :8].contiguous(), df[:2].contiguous()):
+        with pytest.raises(ValueError):
+            m.frames_grad(labels, bad)
     assert by["E"] is None and by["x"].shape == x.shape
     m.close()
 

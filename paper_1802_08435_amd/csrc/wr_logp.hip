@@ -13,6 +13,7 @@
 #include "wr_logp.h"
 #include "wr_ops.h"
 
+#define LR_CAP 64          // classes of a short row that are ranked
 #define LOGP_BLOCKS 2048   // eight blocks of 256 threads a CU
 #define LW_SPLITS 128      // most segments of a row
 #define LW_SEG 8192        // fewest classes of one (but for rounding)
@@ -142,13 +143,13 @@ __device__ __forceinline__ uint32_t group_umin(uint32_t v) {
   return (uint32_t)group_reduce<RT>((int)v, [](int a, int b) { return (int)((uint32_t)a < (uint32_t)b ? (uint32_t)a : (uint32_t)b); });
 }
 
-// One vector's classes c, c + 1, ... in the order of the alternatives (NaN as plain_nan's).  The ones past the
-// row are -inf with numbers past every other, and so come last; ones below `own` are another vector's
-// (key 0).  pop() takes the first away.
+// One vector's classes c, c + 1, ... by their order among the alternatives (NaN as plain_nan's).  Ones below
+// `own` are another vector's and have key 0; ones past the row are -inf with numbers past every other, so they
+// come last (fp32: key 0 for c >= v, if v is given).  sort() puts them in order, pop() takes the first away.
 template <class T>
 struct TopVec {   // 16-bit logits: rank and number in one word, all different, sorted by a merge network (Batcher, 1968)
   uint32_t key[8];
-  __device__ __forceinline__ void init(const float (&z)[8], int c, int own) {
+  __device__ __forceinline__ void keys(const float (&z)[8], int c, int own, int) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       uint32_t u;
@@ -163,6 +164,8 @@ struct TopVec {   // 16-bit logits: rank and number in one word, all different, 
 #pragma unroll
       for (int k = 0; k < 8; ++k)
         if (c + k < own) key[k] = 0;
+  }
+  __device__ __forceinline__ void sort() {
     constexpr int net[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
                                 {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
 #pragma unroll
@@ -188,13 +191,21 @@ struct TopVec {   // 16-bit logits: rank and number in one word, all different, 
 template <>
 struct TopVec<float> {   // sorted by neighbours' exchanges, which keep equal logits in their order
   uint32_t key[4], k_[4];
-  __device__ __forceinline__ void init(const float (&z)[4], int c, int own) {
+  __device__ __forceinline__ void keys(const float (&z)[4], int c, int own, int v) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) key[k] = rank_of(z[k]), k_[k] = k;
+    for (int k = 0; k < 4; ++k) key[k] = rank_of(z[k]);
     if (c < own)
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         if (c + k < own) key[k] = 0;
+    if (v < 1 << 30)   // (the same for all lanes)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k >= v) key[k] = 0;
+  }
+  __device__ __forceinline__ void sort() {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) k_[k] = k;
     constexpr int net[6] = {0, 2, 1, 0, 2, 1};
 #pragma unroll
     for (int i = 0; i < 6; ++i) {
@@ -215,18 +226,47 @@ struct TopVec<float> {   // sorted by neighbours' exchanges, which keep equal lo
   static __device__ __forceinline__ float value(uint32_t key) { return key_value((u64)key << 32); }
 };
 
+// Sum of v over the group's lanes up to this one, and the last lane's.
+template <int RT>
+__device__ __forceinline__ int group_scan(int v, int* last) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  const int lane = threadIdx.x & 63;
+  if constexpr (RT >= 32) {
+    const int t = __shfl(v, (lane & 32) + 15, 64);
+    if (lane & 16) v += t;
+  }
+  if constexpr (RT == 64) {
+    const int t = __builtin_amdgcn_readlane(v, 31);
+    if (lane & 32) v += t;
+  }
+  *last = __shfl(v, lane | (RT - 1), 64);
+  return v;
+}
+
 // Rows of up to RT * E vectors of 16 bytes, in registers: class (e RT + lane) VW + k.
-// Each vector is sorted for itself; then the alternatives are drawn one by one, each
-// lane offering its best class left.  With 16 lanes a row four rows share every
-// reduction of a wave.  48,000 x 256 fp32 (52 MB, 11 us at a copy's rate): 10.7 us
-// without alternatives; with five 17.2, bound by vector instructions (720 for four rows, 60 of
-// them for each alternative).  Widths between the shapes: 24,000 x 512 fp32 in half
-// of a shape for 1,024 took 34 us with five, 19 in its own.
+// Alternatives: each vector is sorted for itself, and then they are drawn one by one,
+// each lane offering its best class left.  With 16 lanes a row four rows share every
+// reduction of a wave.  Where a lane holds four fp32 vectors and up to RT / 2 alternatives
+// are wanted, less is to be done without sorting (48,000 x 256 with five: 18.7 us
+// drawn, 16.6 so; 12,000 x 1,024 with 20: 38 and 24; but bf16, 48,000 x 256 with five, 14.3 and 15.4): the top-th
+// largest of the lanes' best classes is no larger than the top-th largest class, and few
+// classes reach it; those are listed in LDS and ranked among each other, unless they are
+// more than LR_CAP (many equal ones).
+//
+// 48,000 x 256 fp32 (52 MB, 11 us at a copy's rate): 10.7 us without alternatives, 15.7 with
+// five, bound by vector instructions then.  Widths between the shapes have their own:
+// 24,000 x 512 fp32 with five, in half of the shape for 1,024, took 34 us for 17.
 template <class T, int RT, int E, bool TAIL>
 __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
   constexpr int VW = 16 / sizeof(T), KR = (WAVERNN_MAX_TOP + RT - 1) / RT;
   constexpr bool packed = sizeof(T) == 2;
+  constexpr bool LIST = !packed && E == 4;
+  __shared__ u64 lists[LIST ? 256 / RT : 1][LIST ? LR_CAP : 1];
   const int lane = threadIdx.x % RT;
+  u64* list = lists[LIST ? threadIdx.x / RT : 0];
   const int64_t step = (int64_t)gridDim.x * (256 / RT);
   for (int64_t row = (int64_t)blockIdx.x * (256 / RT) + threadIdx.x / RT; row < a.n; row += step) {
     const int64_t t = row_token(a, row), o = row_out(a, row);
@@ -273,8 +313,53 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
       if (q.s != q.s)
 #pragma unroll
         for (int k = 0; k < VW; ++k) z[e][k] = plain_nan(z[e][k]);
-      vec[e].init(z[e], c[e], TAIL ? (e * RT + lane) * VW : c[e]);
+      vec[e].keys(z[e], c[e], TAIL ? (e * RT + lane) * VW : c[e], LIST && a.v < RT * E * VW ? a.v : 1 << 30);
     }
+    if (LIST && a.top <= RT / 2) {
+      uint32_t left = 0, low = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int k = 0; k < VW; ++k) left = max(left, vec[e].key[k]);
+      for (int i = 0; i < a.top; ++i) {   // (lanes whose best are equal go at once, which lowers the bound at most)
+        low = group_umax<RT>(left);
+        left = left == low ? 0 : left;
+      }
+      low = max(low, 1u);
+      int mine = 0, n;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int k = 0; k < VW; ++k) mine += vec[e].key[k] >= low;
+      int to = group_scan<RT>(mine, &n) - mine;
+      if (n <= LR_CAP) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+          for (int k = 0; k < VW; ++k)
+            if (vec[e].key[k] >= low) list[to++] = (u64)vec[e].key[k] << 32 | (uint32_t)~(c[e] + k);
+        __builtin_amdgcn_wave_barrier();   // (a group lies in one wave, whose LDS accesses are in order)
+        for (int i = lane; i < n; i += RT) {
+          const u64 w = list[i];
+          int r = 0;
+          for (int j0 = 0; j0 < n; j0 += 4) {   // (LR_CAP is a multiple of 4)
+            u64 x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = list[j0 + j];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r += j0 + j < n && x[j] > w;
+          }
+          if (r < a.top) {
+            a.top_idx[o * a.top + r] = key_class(w);
+            a.top_logp[o * a.top + r] = key_value(w) - sub;
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
+        continue;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) vec[e].sort();
     uint32_t won[KR] = {}, won_at[KR] = {};
     for (int i = 0; i < a.top; ++i) {
       uint32_t best = vec[0].key[0], at = vec[0].at(c[0]);

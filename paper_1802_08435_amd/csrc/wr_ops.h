@@ -1,5 +1,5 @@
 // Shared by the operators on callers' tensors (wr_logp.hip, wr_embed.hip,
-// wr_norm.hip): element types, row access, reductions, argument checks.
+// wr_norm.hip): element types, row access, argument checks.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -114,22 +114,4 @@ inline int wr_row_threads(int64_t vecs) {
   int t = 1;
   while (t < 256 && t < vecs) t *= 2;
   return t;
-}
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-// Sum over a block of NW waves; every thread gets it.  `s`: NW floats of LDS, free for the next use
-// once every thread has passed the next barrier.
-template <int NW>
-__device__ __forceinline__ float block_sum(float v, float* s) {
-  v = wave_sum(v);
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float r = s[0];
-#pragma unroll
-  for (int i = 1; i < NW; ++i) r += s[i];
-  return r;
 }

@@ -410,7 +410,10 @@ def test_embed_gradient(n, v, d, kind, dt):
 
 
 @pytest.mark.parametrize("n,v,d,kind", [(20000, 3, 64, "even"), (70001, 65537, 32, "skew"), (70001, 255, 16, "sorted"),
-                                        (140000, 1 << 20, 8, "skew"), (300000, 50000, 8, "skew"), (33000, 1, 40, "one")])
+                                        (140000, 1 << 20, 8, "skew"), (300000, 50000, 8, "skew"), (33000, 1, 40, "one"),
+                                        (3000, 700, 48, "skew"), (4096, 100000, 16, "even"), (16000, 5000, 24, "skew"),
+                                        (16384, 300, 7, "sorted"), (200000, 20, 16, "skew"), (500000, 8, 33, "even"),
+                                        (2049, 256, 100, "skew"), (2048, 256, 1000, "one")])
 def test_embed_gradient_many_tokens(n, v, d, kind):
     dout = randn(n, d, seed=1, dt=BF16)
     ids = ids_for(kind, n, v)

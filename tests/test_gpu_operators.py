@@ -611,13 +611,15 @@ def _everything(s, stream=None):
     y, mean, rstd = ops.layer_norm(x, s["gamma"], s["beta"], stats=True, stream=stream)
     dx, dg, db = ops.layer_norm_grad(y, x, mean, rstd, s["gamma"], stream=stream)
     de = ops.embed_grad(dx, s["ids"], s["table"].shape[0], scale=1.5, stream=stream)
-    return [r["logp"], r["entropy"], r["top_logp"], r["top_idx"], big["logp"], big["top_idx"], dz, x, y, dx, dg, db, de]
+    ds = [ops.embed_grad(s["rows"][:n], s["many"][:n], 5000, stream=stream) for n in (3000, 12000, 40000)]
+    return [r["logp"], r["entropy"], r["top_logp"], r["top_idx"], big["logp"], big["top_idx"], dz, x, y, dx, dg, db, de] + ds
 
 
 def _inputs(seed):
     return dict(z=randn(700, 256, seed=seed), t=tokens_for(700, 256, seed=seed), big=randn(2, 90000, seed=seed, dt=BF16),
                 g=randn(700, seed=seed + 1), table=randn(97, 64, seed=seed + 2), ids=tokens_for(2000, 97, seed=seed + 3),
-                gamma=1.0 + randn(64, seed=seed + 4, scale=0.1), beta=randn(64, seed=seed + 5))
+                gamma=1.0 + randn(64, seed=seed + 4, scale=0.1), beta=randn(64, seed=seed + 5),
+                rows=randn(40000, 24, seed=seed + 6, dt=BF16), many=ids_for("skew", 40000, 5000, seed=seed + 7))
 
 
 def test_operators_on_another_stream():
@@ -629,6 +631,18 @@ def test_operators_on_another_stream():
     noise = [torch.full((1 << 20,), 3.0, device="cuda") for _ in range(8)]   # would take freed workspaces
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and len(noise) == 8
+
+
+def test_operators_on_two_streams_at_once():
+    sets = [_inputs(1), _inputs(2)]
+    want = [_everything(s) for s in sets]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[_everything(s, stream=st) for s, st in zip(sets, streams)] for _ in range(4)]
+    torch.cuda.synchronize()
+    for turn in got:
+        for a, b in zip(turn, want):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
 
 
 def test_operators_captured_and_replayed():

@@ -63,9 +63,11 @@ def _rows(name, t):
 
 
 def _plain(name, t, shape, dtypes, device):
-    """t, checked to be contiguous, of the shape, on the device and of one of the dtypes."""
+    """t's address (None for None), t checked to be contiguous, of the shape, on the device and of one of the dtypes."""
+    if t is None:
+        return None
     if t.shape == shape and t.dtype in dtypes and t.device == device and t.is_contiguous():
-        return t
+        return t.data_ptr()
     raise ValueError(f"{name}: needs a contiguous tensor {list(shape)} on {device}, {' or '.join(str(d) for d in dtypes)}; "
                      f"got {t.dtype} {list(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
 
@@ -120,8 +122,7 @@ def token_logprobs(logits, tokens=None, top=0, stream=None):
         return _there(token_logprobs, logits, stream, logits, tokens, top)
     L = _w._lib or _w.lib()
     dt, (n, v, stride), dev, shape = _dtype("logits", logits), _rows("logits", logits), logits.device, logits.shape[:-1]
-    if tokens is not None:
-        _plain("tokens", tokens, shape, _IDS, dev)
+    tokens_p = _plain("tokens", tokens, shape, _IDS, dev)
     ws_bytes = L.wavernn_token_logprobs_workspace(n, v, top)
     ws = _workspace(ws_bytes, logits)
     logp = None
@@ -133,9 +134,9 @@ def token_logprobs(logits, tokens=None, top=0, stream=None):
     if top > 0:
         top_logp = logits.new_empty((*shape, top), dtype=torch.float32)
         top_idx = logits.new_empty((*shape, top), dtype=torch.int32)
-    _w._check(L.wavernn_token_logprobs(dt, _p(logits), n, v, stride, _p(tokens),
-                                       _ID_BYTES[tokens.dtype] if tokens is not None else 0, top, _p(logp),
-                                       _p(entropy), _p(lse), _p(top_logp), _p(top_idx), _p(ws),
+    _w._check(L.wavernn_token_logprobs(dt, logits.data_ptr(), n, v, stride, tokens_p,
+                                       0 if tokens is None else _ID_BYTES[tokens.dtype], top, _p(logp),
+                                       entropy.data_ptr(), lse.data_ptr(), _p(top_logp), _p(top_idx), _p(ws),
                                        max(ws_bytes, 0), _raw_stream(dev.index)))
     return dict(logp=logp, entropy=entropy, lse=lse, top_logp=top_logp, top_idx=top_idx)
 
@@ -151,24 +152,22 @@ def token_logprobs_grad(logits, tokens, lse, entropy=None, g_logp=None, g_entrop
                       g_top, out)
     L = _w._lib or _w.lib()
     dt, (n, v, stride), dev, shape = _dtype("logits", logits), _rows("logits", logits), logits.device, logits.shape[:-1]
-    if tokens is not None:
-        _plain("tokens", tokens, shape, _IDS, dev)
-    for name, t in (("lse", lse), ("entropy", entropy), ("g_logp", g_logp), ("g_entropy", g_entropy), ("g_lse", g_lse)):
-        if t is not None:
-            _plain(name, t, shape, _F32, dev)
-    k = 0
+    tokens_p = _plain("tokens", tokens, shape, _IDS, dev)
+    k, top_p, g_top_p = 0, None, None
     if g_top is not None:
         k = g_top.shape[-1] if g_top.dim() else -1
-        _plain("g_top", g_top, shape + (k,), _F32, dev)
+        g_top_p = _plain("g_top", g_top, shape + (k,), _F32, dev)
         if top_idx is None:
             raise ValueError("g_top needs top_idx")
-        _plain("top_idx", top_idx, shape + (k,), _I32, dev)
+        top_p = _plain("top_idx", top_idx, shape + (k,), _I32, dev)
     out, out_stride = _result("out", out, logits.shape, logits.dtype, logits)
-    _w._check(L.wavernn_token_logprobs_grad(dt, _p(logits), n, v, stride, _p(tokens),
-                                            _ID_BYTES[tokens.dtype] if tokens is not None else 0, _p(lse),
-                                            _p(entropy), _p(g_logp), _p(g_entropy), _p(g_lse), k,
-                                            _p(top_idx) if k else None, _p(g_top), _p(out), out_stride,
-                                            _raw_stream(dev.index)))
+    _w._check(L.wavernn_token_logprobs_grad(dt, logits.data_ptr(), n, v, stride, tokens_p,
+                                            0 if tokens is None else _ID_BYTES[tokens.dtype],
+                                            _plain("lse", lse, shape, _F32, dev), _plain("entropy", entropy, shape, _F32, dev),
+                                            _plain("g_logp", g_logp, shape, _F32, dev),
+                                            _plain("g_entropy", g_entropy, shape, _F32, dev),
+                                            _plain("g_lse", g_lse, shape, _F32, dev), k, top_p, g_top_p, out.data_ptr(),
+                                            out_stride, _raw_stream(dev.index)))
     return out
 
 
@@ -190,11 +189,11 @@ def embed(table, ids, scale=1.0, dtype=None, out=None, stream=None):
     if table.dim() != 2:
         raise ValueError("table: needs two dimensions")
     v, d, stride = _rows("table", table)
-    _plain("ids", ids, ids.shape, _IDS, dev)
+    ids_p = _plain("ids", ids, ids.shape, _IDS, dev)
     dtype = _table_dtype("embed", dtype, table.dtype)
     out, out_stride = _result("out", out, ids.shape + (d,), dtype, table)
-    _w._check(L.wavernn_embed(dt, _p(table), v, d, stride, _p(ids), _ID_BYTES[ids.dtype], ids.numel(), scale,
-                              _DTYPE[dtype], _p(out), out_stride, _raw_stream(dev.index)))
+    _w._check(L.wavernn_embed(dt, table.data_ptr(), v, d, stride, ids_p, _ID_BYTES[ids.dtype], ids.numel(), scale,
+                              _DTYPE[dtype], out.data_ptr(), out_stride, _raw_stream(dev.index)))
     return out
 
 
@@ -206,22 +205,22 @@ def embed_grad(dout, ids, n_rows, scale=1.0, dtype=torch.float32, stream=None):
         return _there(embed_grad, dout, stream, dout, ids, n_rows, scale, dtype)
     L = _w._lib or _w.lib()
     dt, (n, d, stride), dev = _dtype("dout", dout), _rows("dout", dout), dout.device
-    _plain("ids", ids, dout.shape[:-1], _IDS, dev)
+    ids_p = _plain("ids", ids, dout.shape[:-1], _IDS, dev)
     dtype = _table_dtype("embed_grad", dtype, dout.dtype)
     ws_bytes = L.wavernn_embed_grad_workspace(n, d, n_rows)
     ws = _workspace(ws_bytes, dout)
     out = dout.new_empty((max(n_rows, 0), d), dtype=dtype)
-    _w._check(L.wavernn_embed_grad(dt, _p(dout), n, d, stride, _p(ids), _ID_BYTES[ids.dtype], n_rows, scale,
-                                   _DTYPE[dtype], _p(out), _p(ws), max(ws_bytes, 0), _raw_stream(dev.index)))
+    _w._check(L.wavernn_embed_grad(dt, dout.data_ptr(), n, d, stride, ids_p, _ID_BYTES[ids.dtype], n_rows, scale,
+                                   _DTYPE[dtype], out.data_ptr(), _p(ws), max(ws_bytes, 0), _raw_stream(dev.index)))
     return out
 
 
 def _weight(name, w, d, t, other=None):
     if w is None:
-        return
-    _plain(name, w, (d,), (torch.float32, t.dtype), t.device)
+        return None
     if other is not None and w.dtype != other.dtype:
         raise ValueError("gamma and beta must be of one dtype")
+    return _plain(name, w, (d,), (torch.float32, t.dtype), t.device)
 
 
 def layer_norm(x, gamma=None, beta=None, eps=1e-5, stats=False, out=None, stream=None):
@@ -232,15 +231,15 @@ def layer_norm(x, gamma=None, beta=None, eps=1e-5, stats=False, out=None, stream
         return _there(layer_norm, x, stream, x, gamma, beta, eps, stats, out)
     L = _w._lib or _w.lib()
     dt, (n, d, stride), dev = _dtype("x", x), _rows("x", x), x.device
-    _weight("gamma", gamma, d, x)
-    _weight("beta", beta, d, x, gamma)
+    gamma_p = _weight("gamma", gamma, d, x)
+    beta_p = _weight("beta", beta, d, x, gamma)
     w = gamma if gamma is not None else beta
     y, y_stride = _result("out", out, x.shape, x.dtype, x)
     mean = rstd = None
     if stats:
         mean, rstd = x.new_empty((2, *x.shape[:-1]), dtype=torch.float32).unbind()
-    _w._check(L.wavernn_layer_norm(dt, _p(x), n, d, stride, _w.F32 if w is None else _DTYPE[w.dtype], _p(gamma),
-                                   _p(beta), eps, _p(y), y_stride, _p(mean), _p(rstd), _raw_stream(dev.index)))
+    _w._check(L.wavernn_layer_norm(dt, x.data_ptr(), n, d, stride, _w.F32 if w is None else _DTYPE[w.dtype], gamma_p,
+                                   beta_p, eps, y.data_ptr(), y_stride, _p(mean), _p(rstd), _raw_stream(dev.index)))
     return (y, mean, rstd) if stats else y
 
 
@@ -254,9 +253,9 @@ def layer_norm_grad(dy, x, mean, rstd, gamma=None, weights=True, out=None, strea
     dt, (n, d, stride), dev = _dtype("x", x), _rows("x", x), x.device
     if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != dev:
         raise ValueError("dy must be of x's shape, dtype and device")
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        _plain(name, t, x.shape[:-1], _F32, dev)
-    _weight("gamma", gamma, d, x)
+    mean_p = _plain("mean", mean, x.shape[:-1], _F32, dev)
+    rstd_p = _plain("rstd", rstd, x.shape[:-1], _F32, dev)
+    gamma_p = _weight("gamma", gamma, d, x)
     dx, dx_stride = _result("out", out, x.shape, x.dtype, x)
     dgamma = dbeta = ws = None
     ws_bytes = 0
@@ -264,8 +263,8 @@ def layer_norm_grad(dy, x, mean, rstd, gamma=None, weights=True, out=None, strea
         dgamma, dbeta = x.new_empty((2, d), dtype=torch.float32).unbind()
         ws_bytes = L.wavernn_layer_norm_grad_workspace(n, d)
         ws = _workspace(ws_bytes, x)
-    _w._check(L.wavernn_layer_norm_grad(dt, _p(dy), _rows("dy", dy)[2], _p(x), stride, n, d,
-                                        _w.F32 if gamma is None else _DTYPE[gamma.dtype], _p(gamma), _p(mean),
-                                        _p(rstd), _p(dx), dx_stride, _p(dgamma), _p(dbeta),
-                                        _p(ws), max(ws_bytes, 0), _raw_stream(dev.index)))
+    _w._check(L.wavernn_layer_norm_grad(dt, dy.data_ptr(), _rows("dy", dy)[2], x.data_ptr(), stride, n, d,
+                                        _w.F32 if gamma is None else _DTYPE[gamma.dtype], gamma_p, mean_p, rstd_p,
+                                        dx.data_ptr(), dx_stride, _p(dgamma), _p(dbeta), _p(ws), max(ws_bytes, 0),
+                                        _raw_stream(dev.index)))
     return dx, dgamma, dbeta

@@ -322,7 +322,9 @@ wavernn_status wavernn_score_tokens(wavernn_model* m, int32_t n_streams, int64_t
 
 /* Log probability of a given token of each of n_rows distributions, given by
  * logits [n_rows][n_classes], with the entropy and the `top` most likely classes:
- *   lse = log sum_j exp z_j,  logp = z_token - lse,  entropy = - sum_j p_j log p_j,
+ *   lse = log sum_j exp z_j,  logp = z_token - lse,  entropy = - sum_j p_j log p_j
+ *   (logp and top_logp from the differences to the largest logit, so that an offset that all
+ *   logits share costs no digits; lse itself is rounded at its own size),
  *   top_idx, top_logp [n_rows][top]: the classes by falling logit, the lower number first
  *   among equal ones.
  * tokens [n_rows] are whole numbers of token_bytes 4 or 8; a negative one marks a
@@ -343,7 +345,7 @@ wavernn_status wavernn_token_logprobs(int32_t dtype, const void* logits_dev, int
  * g_top [n_rows][top] (of top_logp), each NULL where the loss does not use it,
  *   dlogits_j = [j = token] g_logp + sum_k [j = top_idx_k] g_top_k
  *               + p_j (g_lse - g_logp - sum_k g_top_k) - g_entropy p_j (log p_j + entropy),
- * p_j = exp(z_j - lse), from the forward call's lse, entropy (needed with
+ * p_j = exp(z_j - lse) (off by lse's rounding, 2^-24 |lse| of its value), from the forward call's lse, entropy (needed with
  * g_entropy) and top_idx (needed with top > 0; one that is no class, and its g_top, is
  * ignored).  Rows of padding and rows whose every class is masked are zero whatever
  * the gradients hold there; with g_logp a token of n_classes or more makes its row NaN.  dlogits

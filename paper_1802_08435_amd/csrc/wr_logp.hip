@@ -1,10 +1,12 @@
 // Log probabilities of given tokens with the entropy and the top alternatives
 // of their distributions, and the gradient of all of them with respect to the
 // logits.  For a row z of V logits with m = max z, s = sum e^(z - m):
-//   lse = m + log s,  logp = z_t - lse,
+//   lse = m + log s,  logp = (z_t - m) - log s,
 //   H = -sum p log p = log s - sum (z - m) e^(z - m) / s
 // (both terms of H are >= 0, so nothing cancels), and the top K by (z
-// descending, number ascending).  Sums are fp32.
+// descending, number ascending).  Sums are fp32.  A log probability is formed
+// without lse, whose rounding is the logits' size: at logits near 50 steps of 3.8e-6,
+// which would leave a probable token's -1e-5 one digit.
 //   dz_j = [j = t] g_logp + sum_k [j = top_k] g_top_k
 //        + p_j (g_lse - g_logp - sum_k g_top_k) - g_H p_j (log p_j + H)
 #include <math.h>
@@ -86,15 +88,19 @@ __device__ __forceinline__ void soft_term(float z, float base, float& s, float& 
   s += e;
   w = __builtin_fmaf(fmaxf(d, WR_FAR), e, w);
 }
-// What is taken from a logit for its log probability: log sum exp, or nothing where every class is masked (q.s = 0).
-__device__ __forceinline__ float soft_sub(Soft q) { return q.s == 0.0f ? 0.0f : soft_base(q.m) + logf(q.s); }
+// A row's log probabilities: the logit less the maximum, less log s (nothing where every class is masked, q.s = 0).
+struct LogP {
+  float base, logs;
+  __device__ __forceinline__ float operator()(float z) const { return (z - base) - logs; }
+};
+__device__ __forceinline__ LogP soft_logp(Soft q) { return LogP{soft_base(q.m), q.s == 0.0f ? 0.0f : logf(q.s)}; }
 __device__ __forceinline__ float soft_entropy(Soft q) { return q.s == 0.0f ? 0.0f : logf(q.s) - q.w / q.s; }
 
 template <class T>
-__device__ __forceinline__ void put_row(const LogpArgs& a, int64_t o, int64_t t, const T* z, Soft q, float sub) {
-  if (a.logp) a.logp[o] = t < a.v ? (float)z[t] - sub : __builtin_nanf("");
+__device__ __forceinline__ void put_row(const LogpArgs& a, int64_t o, int64_t t, const T* z, Soft q, LogP lp) {
+  if (a.logp) a.logp[o] = t < a.v ? lp((float)z[t]) : __builtin_nanf("");
   if (a.entropy) a.entropy[o] = soft_entropy(q);
-  if (a.lse) a.lse[o] = q.s == 0.0f ? -__builtin_inff() : sub;
+  if (a.lse) a.lse[o] = q.s == 0.0f ? -__builtin_inff() : lp.base + lp.logs;
 }
 __device__ __forceinline__ void put_padding(const LogpArgs& a, int64_t o, int i) {
   if (i == 0) {
@@ -304,8 +310,8 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
       for (int k = 0; k < VW; ++k) soft_term(z[e][k], base, q.s, q.w);
     q.s = group_fsum<RT>(q.s);
     q.w = group_fsum<RT>(q.w);
-    const float sub = soft_sub(q);
-    if (lane == 0) put_row(a, o, t, zr, q, sub);
+    const LogP lp = soft_logp(q);
+    if (lane == 0) put_row(a, o, t, zr, q, lp);
     if (a.top == 0) continue;
     TopVec<T> vec[E];
 #pragma unroll
@@ -351,7 +357,7 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
           }
           if (r < a.top) {
             a.top_idx[o * a.top + r] = key_class(w);
-            a.top_logp[o * a.top + r] = key_value(w) - sub;
+            a.top_logp[o * a.top + r] = lp(key_value(w));
           }
         }
         __builtin_amdgcn_wave_barrier();
@@ -382,7 +388,7 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
     for (int r = 0; r < KR; ++r)
       if (lane + r * RT < a.top) {
         a.top_idx[o * a.top + lane + r * RT] = TopVec<T>::number(won[r], won_at[r]);
-        a.top_logp[o * a.top + lane + r * RT] = TopVec<T>::value(won[r]) - sub;
+        a.top_logp[o * a.top + lane + r * RT] = lp(TopVec<T>::value(won[r]));
       }
   }
 }
@@ -416,16 +422,16 @@ struct LogpPart {
 };
 
 // Writes alternative k (0 <= k < top) of the row or segment.
-__device__ __forceinline__ void put_top(const LogpArgs& a, int64_t o, int64_t part, int k, u64 key, float sub) {
+__device__ __forceinline__ void put_top(const LogpArgs& a, int64_t o, int64_t part, int k, u64 key, LogP lp) {
   if (a.splits > 1) {
     a.part_keys[part * a.top + k] = key;
   } else {
     a.top_idx[o * a.top + k] = key_class(key);
-    a.top_logp[o * a.top + k] = key_value(key) - sub;
+    a.top_logp[o * a.top + k] = lp(key_value(key));
   }
 }
 // The `top` largest of the n classes listed, in order, by counting the larger ones.
-__device__ __forceinline__ void put_ranked(const LogpArgs& a, LogpShared& sh, int n, int64_t o, int64_t part, float sub) {
+__device__ __forceinline__ void put_ranked(const LogpArgs& a, LogpShared& sh, int n, int64_t o, int64_t part, LogP lp) {
   for (int i = threadIdx.x; i < n; i += 256) {
     const u64 key = sh.list[i];
     int r = 0;
@@ -436,14 +442,14 @@ __device__ __forceinline__ void put_ranked(const LogpArgs& a, LogpShared& sh, in
 #pragma unroll
       for (int j = 0; j < 8; ++j) r += j0 + j < n && x[j] > key;
     }
-    if (r < a.top) put_top(a, o, part, r, key, sub);
+    if (r < a.top) put_top(a, o, part, r, key, lp);
   }
 }
 
 // The alternatives of classes j0 .. j0 + nj - 1, whose vectors the block's threads took in turn.
 template <class T>
 __device__ __forceinline__ void find_top(const LogpArgs& a, LogpShared& sh, const T* z0, int j0, int nj, int vecs, int64_t o,
-                                         int64_t part, float sub) {
+                                         int64_t part, LogP lp) {
   constexpr int VW = 16 / sizeof(T);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   // every wave finds the top-th largest quad for itself, bit by bit
@@ -479,7 +485,7 @@ __device__ __forceinline__ void find_top(const LogpArgs& a, LogpShared& sh, cons
   });
   __syncthreads();
   int n = sh.count;
-  if (n <= LW_CAP) return put_ranked(a, sh, n, o, part, sub);
+  if (n <= LW_CAP) return put_ranked(a, sh, n, o, part, lp);
   // Too many equal or close classes.  Those above `low` alone, and then the first that equal it:
   __syncthreads();
   if (tid == 0) sh.count = 0;
@@ -493,7 +499,7 @@ __device__ __forceinline__ void find_top(const LogpArgs& a, LogpShared& sh, cons
   __syncthreads();
   n = sh.count;
   if (n <= LW_CAP) {
-    put_ranked(a, sh, n, o, part, sub);
+    put_ranked(a, sh, n, o, part, lp);
     int have = n;
     for (int i0 = 0; have < a.top && i0 < vecs; i0 += 256) {
       float z[VW];
@@ -518,7 +524,7 @@ __device__ __forceinline__ void find_top(const LogpArgs& a, LogpShared& sh, cons
 #pragma unroll
       for (int k = 0; k < VW; ++k)
         if (k < count && top_rank(z[k]) == low) {
-          if (r < a.top) put_top(a, o, part, r, top_key(z[k], j0 + c + k), sub);
+          if (r < a.top) put_top(a, o, part, r, top_key(z[k], j0 + c + k), lp);
           ++r;
         }
       __syncthreads();
@@ -542,7 +548,7 @@ __device__ __forceinline__ void find_top(const LogpArgs& a, LogpShared& sh, cons
     if (lane == 0) sh.wave_best[wave] = best;
     __syncthreads();
     for (int w = 0; w < 4; ++w) best = sh.wave_best[w] > best ? sh.wave_best[w] : best;
-    if (tid == 0) put_top(a, o, part, k, best, sub);
+    if (tid == 0) put_top(a, o, part, k, best, lp);
     prev = best;
   }
 }
@@ -605,12 +611,12 @@ __global__ __launch_bounds__(256) void wr_logp_kernel(LogpArgs a) {
     __syncthreads();
     q = soft_join(soft_join(sh.soft[0], sh.soft[1]), soft_join(sh.soft[2], sh.soft[3]));
     if (tid == 0) {
-      if (a.splits == 1) put_row(a, o, t, zr, q, soft_sub(q));
+      if (a.splits == 1) put_row(a, o, t, zr, q, soft_logp(q));
       else ((LogpPart*)a.part)[item].q = q;
     }
     if (a.top > 0) {
-      const float sub = a.splits == 1 ? soft_sub(q) : 0.0f;
-      find_top<T>(a, sh, z0, j0, nj, vecs, o, item, sub);
+      const LogP lp = a.splits == 1 ? soft_logp(q) : LogP{};   // (segments keep the logits)
+      find_top<T>(a, sh, z0, j0, nj, vecs, o, item, lp);
     }
     __syncthreads();
   }
@@ -633,7 +639,8 @@ __global__ __launch_bounds__(256) void wr_logp_join_kernel(LogpArgs a) {
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1)
       q = soft_join(q, Soft{__shfl_xor(q.m, d, 64), __shfl_xor(q.s, d, 64), __shfl_xor(q.w, d, 64)});
-    if (tid == 0) put_row(a, o, t, (const T*)a.logits + row * a.stride, q, soft_sub(q));
+    const LogP lp = soft_logp(q);
+    if (tid == 0) put_row(a, o, t, (const T*)a.logits + row * a.stride, q, lp);
     if (a.top == 0) continue;
     // Each segment's classes come in order, so the top-th largest of their first few (enough that there are
     // `top` of them) is a lower bound, and what reaches it is ranked: with a bound from the best ones alone
@@ -660,7 +667,7 @@ __global__ __launch_bounds__(256) void wr_logp_join_kernel(LogpArgs a) {
     __syncthreads();
     LogpArgs b = a;
     b.splits = 1;
-    put_ranked(b, sh, sh.count, o, 0, soft_sub(q));
+    put_ranked(b, sh, sh.count, o, 0, lp);
     __syncthreads();
   }
 }

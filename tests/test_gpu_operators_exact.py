@@ -1,0 +1,59 @@
+"""The operators on inputs whose sums are exact or short, so that the bounds are a few
+roundings whatever the row's length: a lost or doubled term, and a digit given
+away, show.  u = 2^-24 is fp32's half step.
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_1802_08435_amd import ops  # noqa: E402
+
+U = 2.0 ** -24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+INF = math.inf
+MIX = pytest.mark.parametrize("dt", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+
+
+def within(got, ref, tol, what):
+    err = (got.double() - ref.double()).abs()
+    assert bool((err <= tol).all()), f"{what}: worst {float((err / tol).max()):.3g} times the tolerance"
+
+
+# ---- log probabilities ------------------------------------------------------------
+
+
+@MIX
+@pytest.mark.parametrize("offset", [0.0, 48.0, 1000.0])
+@pytest.mark.parametrize("n,v", [(5, 16), (70, 256), (3, 1000), (2, 2048), (2, 4096), (520, 5000), (1, 70000)])
+def test_log_probabilities_do_not_depend_on_a_common_offset(n, v, offset, dt):
+    """One class 12 ahead of the next and 200 of the others: log P is -6.1e-6 and -12 to the last digits,
+    whatever all logits have in common.  s = 1 + e^-12 is off by two roundings, its logarithm by as much,
+    the differences to the largest logit not at all."""
+    z = torch.full((n, v), offset - 200.0, device="cuda")
+    i = torch.arange(n, device="cuda")
+    a, b = (7 * i + 3) % v, (11 * i + v // 2 + 5) % v
+    b = torch.where(a == b, (b + 1) % v, b)
+    z[i, a], z[i, b] = offset, offset - 12.0
+    z = z.to(dt)
+    zd = z.double()
+    assert bool((zd[i, a] - zd[i, b] == 12.0).all())
+    d = zd - zd.amax(-1, keepdim=True)
+    ref = d - torch.log(torch.exp(d).sum(-1, keepdim=True))
+    for tok in (a, b):
+        for top in {2, 3, min(20, v)}:
+            r = ops.token_logprobs(z, tok, top=top)
+            want = ref[i, tok]
+            within(r["logp"], want, 4 * U + 4 * U * want.abs(), "logp")
+            assert torch.equal(r["top_idx"][:, :2], torch.stack([a, b], 1).int())
+            want = ref.gather(-1, r["top_idx"].long())
+            within(r["top_logp"], want, 4 * U + 4 * U * want.abs(), "top_logp")

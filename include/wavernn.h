@@ -324,7 +324,8 @@ wavernn_status wavernn_score_tokens(wavernn_model* m, int32_t n_streams, int64_t
  * logits [n_rows][n_classes], with the entropy and the `top` most likely classes:
  *   lse = log sum_j exp z_j,  logp = z_token - lse,  entropy = - sum_j p_j log p_j
  *   (logp and top_logp from the differences to the largest logit, so that an offset that all
- *   logits share costs no digits; lse itself is rounded at its own size),
+ *   logits share costs no digits; lse itself is rounded at its own size, and where the largest logit is
+ *   a mask's finite value, past 1e30 in size, lse is that value and logp 0),
  *   top_idx, top_logp [n_rows][top]: the classes by falling logit, the lower number first
  *   among equal ones.
  * tokens [n_rows] are whole numbers of token_bytes 4 or 8; a negative one marks a

@@ -88,12 +88,18 @@ __device__ __forceinline__ void soft_term(float z, float base, float& s, float& 
   s += e;
   w = __builtin_fmaf(fmaxf(d, WR_FAR), e, w);
 }
-// A row's log probabilities: the logit less the maximum, less log s (nothing where every class is masked, q.s = 0).
+// A row's log probabilities: the logit less the maximum, less log s.  Nothing more where every class is masked
+// (q.s = 0), nor where the maximum is a mask's finite value, past WR_MASK in size (the type's lowest): lse is that value
+// itself there, in 64 bits too, and z - lse is 0.
+#define WR_MASK 1e30f
 struct LogP {
   float base, logs;
   __device__ __forceinline__ float operator()(float z) const { return (z - base) - logs; }
 };
-__device__ __forceinline__ LogP soft_logp(Soft q) { return LogP{soft_base(q.m), q.s == 0.0f ? 0.0f : logf(q.s)}; }
+__device__ __forceinline__ LogP soft_logp(Soft q) {
+  const bool none = q.s == 0.0f || (fabsf(q.m) > WR_MASK && q.s == q.s);
+  return LogP{soft_base(q.m), none ? 0.0f : logf(q.s)};
+}
 __device__ __forceinline__ float soft_entropy(Soft q) { return q.s == 0.0f ? 0.0f : logf(q.s) - q.w / q.s; }
 
 template <class T>

@@ -57,3 +57,15 @@ def test_log_probabilities_do_not_depend_on_a_common_offset(n, v, offset, dt):
             assert torch.equal(r["top_idx"][:, :2], torch.stack([a, b], 1).int())
             want = ref.gather(-1, r["top_idx"].long())
             within(r["top_logp"], want, 4 * U + 4 * U * want.abs(), "top_logp")
+
+
+def test_log_probabilities_of_rows_at_a_mask_s_value():
+    """Every class at fp32's lowest or largest value: lse is that value, logp 0, the entropy log V; with a +inf, NaN."""
+    for v in (16, 256, 5000, 70000):
+        z = torch.stack([torch.full((v,), x, device="cuda") for x in (torch.finfo(F32).min, torch.finfo(F32).max, 1e29)])
+        z[2, 1:] = INF
+        r = ops.token_logprobs(z, torch.zeros(3, dtype=torch.int64, device="cuda"), top=3)
+        assert torch.equal(r["lse"][:2], z[:2, 0]) and torch.equal(r["logp"][:2], torch.zeros(2, device="cuda"))
+        assert torch.equal(r["top_logp"][:2], torch.zeros(2, 3, device="cuda"))
+        within(r["entropy"][:2], torch.full((2,), math.log(v), device="cuda"), 4 * U * math.log(v), "entropy")
+        assert all(bool(torch.isnan(r[k][2]).all()) for k in ("logp", "entropy", "lse", "top_logp"))

@@ -378,13 +378,15 @@ wavernn_status wavernn_embed_grad(int32_t dout_dtype, const void* dout_dev, int6
 /* Layer norm of rows of `dim` elements: y = (x - mean) rstd gamma + beta with the
  * row's mean and rstd = 1 / sqrt(variance + eps), eps > 0.  gamma, beta [dim] are of
  * w_dtype (x's type or F32), NULL = 1 and 0.  mean, rstd [n_rows] (NULL: not
- * wanted) are what the gradient needs.  y may be x (same stride).  Elements past about 1e18 overflow
+ * wanted) are what the gradient needs.  The mean's own rounding is centred away: a row far from 0
+ * keeps the digits of its spread.  y may be x (same stride).  Elements past about 1e18 overflow
  * the fp32 variance. */
 wavernn_status wavernn_layer_norm(int32_t dtype, const void* x_dev, int64_t n_rows, int32_t dim, int64_t x_stride,
                                   int32_t w_dtype, const void* gamma_dev, const void* beta_dev, float eps, void* y_dev,
                                   int64_t y_stride, float* mean_dev, float* rstd_dev, void* stream);
 /* Its gradient: dx (of x's type; may be dy or x, same stride), dgamma and dbeta
- * [dim] fp32, summed over the rows; each NULL where not wanted.  The workspace is
+ * [dim] fp32, summed over the rows; each NULL where not wanted.  x - mean carries the given mean's
+ * rounding, 2^-24 of the mean.  The workspace is
  * for dgamma and dbeta. */
 int64_t wavernn_layer_norm_grad_workspace(int64_t n_rows, int32_t dim);
 wavernn_status wavernn_layer_norm_grad(int32_t dtype, const void* dy_dev, int64_t dy_stride, const void* x_dev,

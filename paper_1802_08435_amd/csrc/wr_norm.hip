@@ -3,8 +3,10 @@
 //   y = (x - m) r gamma + beta
 // and with h = (x - m) r, g = dy gamma:
 //   dx = r (g - mean g - h mean (g h)),  dgamma = sum_rows dy h,  dbeta = sum_rows dy.
-// Statistics and sums are fp32; the variance is taken about the mean, so a
-// large mean costs no digits.
+// Statistics and sums are fp32.  The sum's mean m' is off by some roundings of the row's size, which for a
+// row far from 0 could be more than its spread (a constant row at 3e5 could come out as +-1 for 0), so
+// forward the differences c = x - m' are centred once more: m = m' + mean c, v = mean c^2 - (mean c)^2,
+// y = (c - mean c) r gamma + beta.  Backward x - m is as good as the mean given, half an fp32 step of it.
 //
 // Both are bound by memory (forward one read and one write of the rows,
 // backward two and one), so a row is read once and kept in registers between its
@@ -41,11 +43,17 @@ struct NormArgs {
   float *mean, *rstd;
 };
 
+// Sum over the wave's lanes of a row, in every one of them: within 16 lanes by rotations, which need no LDS and
+// pair the same operands as exchanges would (the second sum of the differences cost 1.2 us of 65,536 x 256 fp32 by those).
+template <int N>
+__device__ __forceinline__ float rotate_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + N, 0xf, 0xf, true));
+}
 template <int RT>
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int o = (RT < 64 ? RT : 64) / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  if constexpr (RT > 32) v += __shfl_xor(v, 32, 64);
+  if constexpr (RT > 16) v += __shfl_xor(v, 16, 64);
+  return rotate_add<1>(rotate_add<2>(rotate_add<4>(rotate_add<8>(v))));
 }
 // Sums of K values over the RT threads of a row; `s` (RT > 64): [waves of the block][K], another one for the next sum.
 template <int RT, int K>
@@ -65,6 +73,12 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float* s) {
       for (int w = 1; w < RT / 64; ++w) v[k] += s[w * K + k];
     }
   }
+}
+
+// 1 / sqrt(variance + eps) from the mean square and the mean of the differences.
+__device__ __forceinline__ float norm_rstd(float square, float dm, float eps) {
+  const float v = square - dm * dm;
+  return 1.0f / sqrtf((v < 0.0f ? 0.0f : v) + eps);   // (a NaN stays)
 }
 
 // Columns of thread t's vector e: where it begins, how many of its first elements are not its own
@@ -97,7 +111,7 @@ struct NormCols {
 template <class T, class W, int RT, int E>
 __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_kernel(NormArgs a) {
   constexpr int VW = 16 / sizeof(T), BT = RT < 256 ? 256 : RT, G = BT / RT;
-  __shared__ float red[2][BT / 64];
+  __shared__ float red[2][BT / 64 * 2];
   const int t = threadIdx.x % RT;
   const float inv_d = 1.0f / (float)a.d;
   Raw<W, VW> ga[E], be[E];
@@ -128,26 +142,27 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_kernel(NormArgs a
     }
     row_sums<RT, 1>(s, red[0]);
     const float m = s[0] * inv_d;
-    s[0] = 0.0f;
+    float c[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const NormCols<RT, VW> q(e, t, a.d);
 #pragma unroll
       for (int k = 0; k < VW; ++k) v[e][k] -= m;
-      s[0] += q.sum([&](int k, float s) { return __builtin_fmaf(v[e][k], v[e][k], s); });
+      c[0] += q.sum([&](int k, float s) { return s + v[e][k]; });
+      c[1] += q.sum([&](int k, float s) { return __builtin_fmaf(v[e][k], v[e][k], s); });
     }
-    row_sums<RT, 1>(s, red[1]);
-    const float r = 1.0f / sqrtf(s[0] * inv_d + a.eps);
+    row_sums<RT, 2>(c, red[1]);
+    const float dm = c[0] * inv_d, r = norm_rstd(c[1] * inv_d, dm, a.eps);
     if (on) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const NormCols<RT, VW> q(e, t, a.d);
 #pragma unroll
-        for (int k = 0; k < VW; ++k) v[e][k] = __builtin_fmaf(v[e][k] * r, (float)ga[e][k], (float)be[e][k]);
+        for (int k = 0; k < VW; ++k) v[e][k] = __builtin_fmaf((v[e][k] - dm) * r, (float)ga[e][k], (float)be[e][k]);
         store_part<T, VW>(y + q.c, v[e], q.count);
       }
       if (t == 0) {
-        if (a.mean) a.mean[i] = m;
+        if (a.mean) a.mean[i] = m + dm;
         if (a.rstd) a.rstd[i] = r;
       }
     }
@@ -158,7 +173,7 @@ __global__ __launch_bounds__(RT < 256 ? 256 : RT) void wr_norm_kernel(NormArgs a
 template <class T, class W>
 __global__ __launch_bounds__(1024) void wr_norm_wide_kernel(NormArgs a) {
   constexpr int VW = 16 / sizeof(T), RT = 1024;
-  __shared__ float red[2][RT / 64];
+  __shared__ float red[2][RT / 64 * 2];
   for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
     const T* x = (const T*)a.x + i * a.x_stride;
     T* y = (T*)a.y + i * a.y_stride;
@@ -170,15 +185,15 @@ __global__ __launch_bounds__(1024) void wr_norm_wide_kernel(NormArgs a) {
     }
     row_sums<RT, 1>(s, red[0]);
     const float m = s[0] / (float)a.d;
-    s[0] = 0.0f;
+    float cs[2] = {0.0f, 0.0f};
     for (int64_t c = threadIdx.x * VW; c < a.d; c += RT * VW) {
       load_part<T, VW>(x + c, v, (int)(a.d - c));
 #pragma unroll
       for (int k = 0; k < VW; ++k)
-        if (c + k < a.d) s[0] = __builtin_fmaf(v[k] - m, v[k] - m, s[0]);
+        if (c + k < a.d) cs[0] += v[k] - m, cs[1] = __builtin_fmaf(v[k] - m, v[k] - m, cs[1]);
     }
-    row_sums<RT, 1>(s, red[1]);
-    const float r = 1.0f / sqrtf(s[0] / (float)a.d + a.eps);
+    row_sums<RT, 2>(cs, red[1]);
+    const float dm = cs[0] / (float)a.d, r = norm_rstd(cs[1] / (float)a.d, dm, a.eps);
     for (int64_t c = threadIdx.x * VW; c < a.d; c += RT * VW) {
       const int count = (int)(a.d - c);
       float ga[VW], be[VW];
@@ -188,11 +203,11 @@ __global__ __launch_bounds__(1024) void wr_norm_wide_kernel(NormArgs a) {
       if (a.beta) load_part<W, VW>((const W*)a.beta + c, be, count);
       load_part<T, VW>(x + c, v, count);
 #pragma unroll
-      for (int k = 0; k < VW; ++k) v[k] = __builtin_fmaf((v[k] - m) * r, ga[k], be[k]);
+      for (int k = 0; k < VW; ++k) v[k] = __builtin_fmaf((v[k] - m - dm) * r, ga[k], be[k]);
       store_part<T, VW>(y + c, v, count);
     }
     if (threadIdx.x == 0) {
-      if (a.mean) a.mean[i] = m;
+      if (a.mean) a.mean[i] = m + dm;
       if (a.rstd) a.rstd[i] = r;
     }
   }

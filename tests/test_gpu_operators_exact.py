@@ -69,3 +69,50 @@ def test_log_probabilities_of_rows_at_a_mask_s_value():
         assert torch.equal(r["top_logp"][:2], torch.zeros(2, 3, device="cuda"))
         within(r["entropy"][:2], torch.full((2,), math.log(v), device="cuda"), 4 * U * math.log(v), "entropy")
         assert all(bool(torch.isnan(r[k][2]).all()) for k in ("logp", "entropy", "lse", "top_logp"))
+
+
+# ---- layer norm ------------------------------------------------------------
+
+
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}
+WIDTHS = [33, 64, 257, 1000, 2048, 4099, 9000, 20001]
+
+
+def depth(d):
+    """Roundings on an element's way into a row's sum: up to 32 columns a thread, wide rows d / 1,024, and the threads'."""
+    return max(32, d // 1024 + 8) + 16
+
+
+@MIX
+@pytest.mark.parametrize("d", WIDTHS)
+def test_rows_far_from_zero_keep_the_digits_of_their_spread(d, dt):
+    """Steps of the type at 10,000 (fp32) or 1,024: x - m' is exact, so the result is off by the differences' sums
+    alone, whose size is the spread's and the first mean's error e = depth u |x|."""
+    off, step = {F32: (1e4, 0.125), F16: (1024.0, 1.0), BF16: (1024.0, 8.0)}[dt]
+    g = torch.Generator(device="cuda").manual_seed(d)
+    x = (off + step * torch.randint(0, 9, (7, d), generator=g, device="cuda")).to(dt)
+    xd = x.double()
+    m = xd.mean(-1, keepdim=True)
+    var = ((xd - m) ** 2).mean(-1, keepdim=True)
+    r = 1.0 / torch.sqrt(var + 1e-5)
+    h = (xd - m) * r
+    k, e = depth(d), depth(d) * U * off
+    size = var.sqrt() + e
+    rel = (k + 8) * U * 2 * (var + e * e) / (var + 1e-5) + 4 * U
+    y, mean, rstd = ops.layer_norm(x, stats=True)
+    within(y, h, (k + 4) * U * size * r + 2 * U * (h.abs() + e * r) + h.abs() * rel + HALF[dt] * h.abs() * 1.001 + 2.0 ** -25,
+           "y")
+    within(mean, m[:, 0], U * off + (k + 4) * U * size[:, 0], "mean")
+    within(rstd, r[:, 0], r[:, 0] * rel[:, 0], "rstd")
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+def test_constant_rows_are_beta_wherever_they_lie(d):
+    """Variance 0: what is left of x - m is (depth u) of the first mean's error depth u |x|, times 1 / sqrt(eps)."""
+    for c in (0.1, 1e3 / 3, 1e6 / 3):
+        beta = torch.arange(float(d), device="cuda")
+        y, mean, rstd = ops.layer_norm(torch.full((3, d), c, device="cuda"), None, beta, eps=1e-5, stats=True)
+        x = float(torch.tensor(c, dtype=F32))
+        e = (depth(d) + 4) * U
+        within(y, beta, e * e * x * 1e-5 ** -0.5 + 2 * U * beta.abs(), "y")
+        within(mean, torch.full_like(mean, x), 2 * U * x, "mean")

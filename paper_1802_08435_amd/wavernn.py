@@ -370,15 +370,17 @@ class Model:
     def score_tokens(self, target, cond=None, init=None, top: int = 0, stream=None, labels=None):
         """Teacher-forced scoring of target [S][T] uint16 by its distributions instead of their logits:
         a dict of logp and entropy [S][T][J] (J = 2: coarse and fine byte; fused: 4, the high and
-        low nibble of each) and, with top > 0, top_logp and top_idx [S][T][J][top] (else None)."""
+        low nibble of each) and, with top > 0, top_logp and top_idx [S][T][J][top] (else None).  The
+        results belong to ``stream``, as ops' do."""
         import torch
         S, T = target.shape
         J = 4 if self.fused else 2
         cond = self._cond(cond, labels, stream)
-        logp, entropy = (torch.empty(S, T, J, device="cuda") for _ in range(2))
         k = max(int(top), 0)
-        top_logp = torch.empty(S, T, J, k, device="cuda") if k else None
-        top_idx = torch.empty(S, T, J, k, dtype=torch.int32, device="cuda") if k else None
+        with torch.cuda.stream(stream):
+            logp, entropy = (torch.empty(S, T, J, device="cuda") for _ in range(2))
+            top_logp = torch.empty(S, T, J, k, device="cuda") if k else None
+            top_idx = torch.empty(S, T, J, k, dtype=torch.int32, device="cuda") if k else None
         n_frames = 0 if cond is None else cond.shape[1]
         si = self._state(init)
         _check(lib().wavernn_score_tokens(self._h, S, T, _ptr(cond), n_frames, _ptr(target),

@@ -171,3 +171,28 @@ def test_a_front_end_that_does_not_fit_is_refused():
     with pytest.raises(ValueError, match="label table"):
         m.frames(torch.zeros(1, 4, dtype=torch.int64, device="cuda"))
     m.close()
+
+
+def test_score_tokens_on_another_stream_owns_its_results_there():
+    """Results dropped on the host while the side stream may still write them: their memory is
+    the side stream's, and what the current stream allocates next lies elsewhere."""
+    w = synth.make_weights(128, seed=7)
+    m = wavernn.Model(w, max_streams=2)
+    tgt = cuda(synth.target_signal(2, 20000, seed=8, kind="uniform"))
+    want = m.score_tokens(tgt, top=8)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.empty_cache()
+    got = m.score_tokens(tgt, top=8, stream=side)
+    sizes = [(t.shape, t.dtype) for t in got.values()]
+    spans = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in got.values()]
+    keep = m.score_tokens(tgt, top=8, stream=side)
+    del got
+    fresh = [torch.full(s, 7, dtype=d, device="cuda") for s, d in sizes]
+    for t in fresh:
+        for lo, hi in spans:
+            assert t.data_ptr() + t.numel() * t.element_size() <= lo or hi <= t.data_ptr(), "memory of the side stream reused"
+    side.synchronize()
+    assert all(torch.equal(keep[k], want[k]) for k in want)
+    m.device_status()
+    m.close()

@@ -210,20 +210,44 @@ class Model:
         if x.dtype.is_floating_point:
             self._check_frames("features", x)
             return x
+        x = self._labels(x)
+        return ops.embed(self.E, x, scale=self.E_scale, stream=stream).view(x.shape[0], x.shape[1], self.cond_dim)
+
+    def _labels(self, x):
+        """Labels as [S][n_frames][cond_dim / d]."""
         if self.E is None:
             raise ValueError("labels need a model with a label table (E)")
-        d = self.E.shape[1]
-        fields = self.cond_dim // d
+        fields = self.cond_dim // self.E.shape[1]
         if x.dim() == 2:
             x = x.unsqueeze(-1)
         if x.dim() != 3 or x.shape[2] != fields:
             raise ValueError(f"labels must be [S][n_frames][{fields}], got {list(x.shape)}")
-        return ops.embed(self.E, x, scale=self.E_scale, stream=stream).view(x.shape[0], x.shape[1], self.cond_dim)
+        return x
 
     def _check_frames(self, name, x):
         import torch
-        if x.dim() != 3 or x.shape[2] != self.cond_dim or x.dtype != torch.float32 or not x.is_contiguous():
-            raise ValueError(f"{name} must be contiguous float32 [S][n_frames][{self.cond_dim}], got {x.dtype} {list(x.shape)}")
+        if x.dim() != 3 or x.shape[2] != self.cond_dim or x.dtype != torch.float32 or not x.is_contiguous() or not x.is_cuda:
+            raise ValueError(f"{name} must be contiguous float32 [S][n_frames][{self.cond_dim}] on the GPU, "
+                             f"got {x.dtype} {list(x.shape)} on {x.device}")
+
+    def _check_scored(self, target, cond, init):
+        """target, cond and init of a score_tokens call: the library gets addresses only."""
+        import torch
+        if target.dim() != 2 or target.dtype != torch.uint16 or not target.is_contiguous() or not target.is_cuda:
+            raise ValueError(f"target must be contiguous uint16 [S][T] on the GPU, got {target.dtype} {list(target.shape)} "
+                             f"on {target.device}")
+        S, dev = target.shape[0], target.device
+        if cond is not None and self.cond_dim > 0:
+            self._check_frames("cond", cond)
+            if cond.shape[0] != S or cond.device != dev:
+                raise ValueError(f"cond holds {cond.shape[0]} utterances on {cond.device}, target {S} on {dev}")
+        if init is not None:
+            rows = S if self.fused else S * self.B
+            for k, dtype, n in (("h", torch.float32, rows * self.H), ("c", torch.uint8, S * self.B), ("f", torch.uint8, S * self.B)):
+                t = init[k]
+                if t.dtype != dtype or t.numel() < n or not t.is_contiguous() or t.device != dev:
+                    raise ValueError(f"init's {k} must be contiguous {dtype} of {n} elements on {dev}, "
+                                     f"got {t.dtype} {list(t.shape)} on {t.device}")
 
     def frames(self, x, stream=None):
         """Conditioning frames [S][n_frames][cond_dim] fp32, as sample and score take them, through the
@@ -243,7 +267,11 @@ class Model:
         self._check_frames("dframes", dframes)
         if dframes.shape[:2] != x.shape[:2]:
             raise ValueError(f"dframes {list(dframes.shape)} and x {list(x.shape)} must have the same frames")
-        labels = None if x.dtype.is_floating_point else x
+        labels = None
+        if x.dtype.is_floating_point:
+            self._check_frames("features", x)
+        else:
+            labels = self._labels(x)
         grads = dict(E=None, ln_g=None, ln_b=None, x=None)
         d = dframes
         if self.ln_g is not None or self.ln_b is not None:
@@ -255,18 +283,18 @@ class Model:
         if labels is None:
             grads["x"] = d
         else:
-            if self.E is None:
-                raise ValueError("labels need a model with a label table (E)")
-            labels = labels.unsqueeze(-1) if labels.dim() == 2 else labels
             grads["E"] = ops.embed_grad(d.view(*labels.shape, self.E.shape[1]), labels, self.E.shape[0],
                                         scale=self.E_scale, stream=stream)
         return grads
 
-    def _cond(self, cond, labels, stream):
+    def _cond(self, cond, labels, stream, n_streams):
+        """Frames of a call on n_streams utterances (the library reads that many, whatever cond holds)."""
         if labels is None:
             return cond
         if cond is not None:
             raise ValueError("cond and labels given: one of the two")
+        if labels.dim() == 0 or labels.shape[0] != n_streams:
+            raise ValueError(f"labels {list(labels.shape)} are not of the call's {n_streams} utterances")
         return self.frames(labels, stream)
 
     def close(self):
@@ -316,7 +344,7 @@ class Model:
         import torch
         if noalloc and labels is not None:
             raise ValueError("sample(noalloc=True) takes frames (cond), not labels")
-        cond = self._cond(cond, labels, stream)
+        cond = self._cond(cond, labels, stream, n_streams)
         if out is None:
             if noalloc:
                 raise ValueError("sample(noalloc=True) needs a preallocated out tensor")
@@ -343,7 +371,7 @@ class Model:
         new_state, required when step0 > 0); final receives the state after the
         last step (include/wavernn.h, wavernn_sample_steps)."""
         S, n_samples = out.shape
-        cond = self._cond(cond, labels, stream)
+        cond = self._cond(cond, labels, stream, S)
         n_frames = 0 if cond is None else cond.shape[1]
         si, sf = self._state(init), self._state(final)
         _check(lib().wavernn_sample_steps(self._h, S, n_samples, _ptr(cond), n_frames, seed, step0, n_steps,
@@ -356,7 +384,7 @@ class Model:
         import torch
         S, T = target.shape
         nz = 32 if self.fused else 256
-        cond = self._cond(cond, labels, stream)
+        cond = self._cond(cond, labels, stream, S)
         zc = torch.empty(S, T, nz, device="cuda") if logits else None
         zf = torch.empty(S, T, nz, device="cuda") if logits else None
         nl = torch.empty(S, T, device="cuda") if nll else None
@@ -373,9 +401,10 @@ class Model:
         low nibble of each) and, with top > 0, top_logp and top_idx [S][T][J][top] (else None).  The
         results belong to ``stream``, as ops' do."""
         import torch
+        self._check_scored(target, cond, init)
         S, T = target.shape
         J = 4 if self.fused else 2
-        cond = self._cond(cond, labels, stream)
+        cond = self._cond(cond, labels, stream, S)
         k = max(int(top), 0)
         with torch.cuda.stream(stream):
             logp, entropy = (torch.empty(S, T, J, device="cuda") for _ in range(2))

@@ -278,7 +278,9 @@ wavernn_status wavernn_sample_noalloc(wavernn_model* m, int32_t n_streams, int64
  * output layers run over all steps as matrix-core GEMMs.  That path keeps h of every step (4 H bytes per sample)
  * and the output layers' intermediates (4 (Hh rounded up to 128) + 2 KiB per
  * sample, for at most 65,536 samples at a time) in model-owned buffers, grown
- * the first time a longer call needs them; its initial state, conditioning
+ * the first time a longer call needs them (to twice their size if that is
+ * more; replaced ones are kept until the model is destroyed, so that a model keeps at most
+ * four times what its longest call needs); its initial state, conditioning
  * and outputs are as above. */
 wavernn_status wavernn_score_teacher_forced(wavernn_model* m, int32_t n_streams, int64_t n_samples,
                                             const float* cond_dev, int64_t n_frames, const uint16_t* target_dev,
@@ -296,7 +298,7 @@ wavernn_status wavernn_score_teacher_forced(wavernn_model* m, int32_t n_streams,
  * top pointers may be NULL.  A dense model on the multi-workgroup persistent path
  * keeps the logits of 65,536 samples at a time; the other models those of the
  * whole call, in a model-owned buffer (2 KiB, fused 256 bytes, per sample), grown
- * the first time a longer call needs it.  Errors: as
+ * and kept likewise.  Errors: as
  * wavernn_score_teacher_forced. */
 wavernn_status wavernn_score_tokens(wavernn_model* m, int32_t n_streams, int64_t n_samples, const float* cond_dev,
                                     int64_t n_frames, const uint16_t* target_dev, const wavernn_state* init, int32_t top,

@@ -168,7 +168,7 @@ struct wavernn_model {
   float* d_tz = nullptr;              // [2][samples] logits of a wavernn_score_tokens call on the other paths
   int64_t tz_cap = 0;                 // its floats
   uint16_t* d_zero = nullptr;         // 128 bytes of zeros (GEMM rows read as zero)
-  int64_t so_cap = 0;                       // rows of d_so and d_sz (at most one chunk of the output layers)
+  int64_t so_cap = 0, sz_cap = 0;           // rows of d_so and d_sz (at most one chunk of the output layers)
   u64* trace = nullptr;
   int64_t trace_steps = 0;
   // a few utterances side by side, each on its own batch-1 grid and stream, all grids co-resident at once
@@ -230,6 +230,18 @@ struct wavernn_model {
     allocs.push_back(q);
     *p = (T*)q;
     return WAVERNN_OK;
+  }
+  // Room for `need` units in a scoring buffer of `cap`, `unit` bytes each.  The old buffer stays allocated
+  // until the model is destroyed (a captured call may hold its address), so a new one has twice its room (`most`
+  // units at most): whatever lengths calls come in, all that is kept is at most twice the newest buffer.
+  template <typename T>
+  wavernn_status grow(T** p, int64_t* cap, int64_t need, size_t unit, int64_t most = INT64_MAX) {
+    if (need <= *cap) return WAVERNN_OK;
+    int64_t n = std::max(need, std::min(2 * *cap, most));
+    wavernn_status s = alloc(p, (size_t)n * unit);
+    if (s == WAVERNN_E_OOM && n > need) s = alloc(p, (size_t)(n = need) * unit);
+    if (s == WAVERNN_OK) *cap = n;
+    return s;
   }
   template <typename T>
   wavernn_status upload(T** p, const void* host, size_t bytes) {
@@ -1733,20 +1745,13 @@ wavernn_status run_score(wavernn_model* m, const RunIO& io) {
   const int H = m->plan.H, Dc = m->cfg.cond_dim, NW = H / 32;
   const int LV = io.S <= 8 ? 1 : io.S <= 16 ? 2 : io.S <= 32 ? 4 : 8, G = (io.S + LV - 1) / LV;
   const int64_t cbf = (int64_t)io.S * n_cb * 3 * H;
-  if (rows > m->traj_cap || (post && ch > m->so_cap) || cbf > m->scb_cap) HIPOK(hipStreamSynchronize(io.st));
+  if (rows > m->traj_cap || (post && (ch > m->so_cap || ch > m->sz_cap)) || cbf > m->scb_cap) HIPOK(hipStreamSynchronize(io.st));
   wavernn_status st;
-  if (cbf > m->scb_cap) {
-    if ((st = m->alloc(&m->d_scb, (size_t)cbf * 4)) != WAVERNN_OK) return st;
-    m->scb_cap = cbf;
-  }
-  if (rows > m->traj_cap) {
-    if ((st = m->alloc(&m->d_traj, (size_t)2 * rows * Hh * 4)) != WAVERNN_OK) return st;
-    m->traj_cap = rows;
-  }
-  if (post && ch > m->so_cap) {   // (a replaced buffer stays allocated until the model is destroyed)
-    if ((st = m->alloc(&m->d_so, (size_t)ch * NP * 4)) != WAVERNN_OK) return st;
-    if ((st = m->alloc(&m->d_sz, (size_t)2 * ch * 256 * 4)) != WAVERNN_OK) return st;
-    m->so_cap = ch;
+  if ((st = m->grow(&m->d_scb, &m->scb_cap, cbf, 4)) != WAVERNN_OK) return st;
+  if ((st = m->grow(&m->d_traj, &m->traj_cap, rows, (size_t)2 * Hh * 4)) != WAVERNN_OK) return st;
+  if (post) {
+    if ((st = m->grow(&m->d_so, &m->so_cap, ch, (size_t)NP * 4, CH)) != WAVERNN_OK) return st;
+    if ((st = m->grow(&m->d_sz, &m->sz_cap, ch, (size_t)2 * 256 * 4, CH)) != WAVERNN_OK) return st;
   }
   if ((st = launch_cond(m, io.cond, n_cb, first_frame(m, io), last_frame(m, io), io.S, m->d_scb, 0, nullptr, 0, 0,
                         io.st)) != WAVERNN_OK)
@@ -2302,8 +2307,7 @@ wavernn_status wavernn_score_tokens(wavernn_model* m, int32_t n_streams, int64_t
     HIPOK(hipGetDevice(&dev));
     if (dev != m->device) return fail(WAVERNN_E_INVALID, "model lives on device %d, current device is %d", m->device, dev);
     HIPOK(hipStreamSynchronize(st));
-    if ((s = m->alloc(&m->d_tz, (size_t)(2 * rows * nz) * 4)) != WAVERNN_OK) return s;
-    m->tz_cap = 2 * rows * nz;
+    if ((s = m->grow(&m->d_tz, &m->tz_cap, 2 * rows * nz, 4)) != WAVERNN_OK) return s;
   }
   io.zc = m->d_tz;
   io.zf = m->d_tz + rows * nz;

@@ -196,3 +196,32 @@ def test_score_tokens_on_another_stream_owns_its_results_there():
     assert all(torch.equal(keep[k], want[k]) for k in want)
     m.device_status()
     m.close()
+
+
+@pytest.mark.parametrize("kind", ["sparse", "dense"])
+def test_scoring_rising_lengths_keeps_a_bounded_memory(kind):
+    """Utterances of 1, 2, ... 24 thousand samples: what the model holds at the end is at most four times the longest
+    call's share (all calls' shares would be 12.5 times that)."""
+    if kind == "sparse":
+        m = wavernn.Model(synth.make_weights(256, seed=3, block=(4, 4), density=0.1), r_format="bsr4x4")
+        share = 2048
+    else:
+        m = wavernn.Model(synth.make_weights(256, seed=2))
+        share = 4 * 256 + 4 * 128 + 2048
+    tgt = cuda(synth.target_signal(1, 24000, seed=6, kind="uniform"))
+    m.score_tokens(tgt[:, :100].contiguous())
+    torch.cuda.synchronize()
+
+    def held():   # outside torch's own pool
+        free, total = torch.cuda.mem_get_info()
+        return total - free - torch.cuda.memory_reserved()
+
+    before = held()
+    for n in range(1000, 24001, 1000):
+        m.score_tokens(tgt[:, :n].contiguous())
+    m.device_status()
+    last = m.score_tokens(tgt)
+    # (2 MiB: the granularity of each of a few allocations)
+    assert held() - before <= 4 * share * 24000 + 16 * (2 << 20)
+    assert torch.equal(m.score_tokens(tgt[:, :1000].contiguous())["logp"], last["logp"][:, :1000])
+    m.close()

@@ -375,22 +375,27 @@ __global__ __launch_bounds__(256) void wr_norm_wide_dw_kernel(NormGradArgs a) {
   store_part<float, 4>(pb + c, db, pb ? count : 0);
 }
 
-// The parts of 64 sums added: each of 16 waves every 16th part, then the waves in order.
+// The parts of 64 sums added: each of 16 waves every 16th part, then the waves in order.  (Blocks stride over
+// the sums: a block each would pass the grid limit from 2^27 columns on.)
 __global__ __launch_bounds__(1024) void wr_norm_parts_kernel(NormGradArgs a) {
   __shared__ float sum[16][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane, n = 2 * (int64_t)a.d;
-  float s = 0.0f;
-  if (c < n)
+  const int64_t n = 2 * (int64_t)a.d;
+  for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < n; c0 += (int64_t)gridDim.x * 64) {
+    const int64_t c = c0 + lane;
+    float s = 0.0f;
+    if (c < n)
 #pragma unroll 8
-    for (int p = w; p < a.parts; p += 16) s += a.part[(int64_t)p * n + c];
-  sum[w][lane] = s;
-  __syncthreads();
-  if (w == 0 && c < n) {
+      for (int p = w; p < a.parts; p += 16) s += a.part[(int64_t)p * n + c];
+    sum[w][lane] = s;
+    __syncthreads();
+    if (w == 0 && c < n) {
 #pragma unroll
-    for (int q = 1; q < 16; ++q) s += sum[q][lane];
-    float* o = c < a.d ? a.dgamma : a.dbeta;
-    if (o) o[c < a.d ? c : c - a.d] = s;
+      for (int q = 1; q < 16; ++q) s += sum[q][lane];
+      float* o = c < a.d ? a.dgamma : a.dbeta;
+      if (o) o[c < a.d ? c : c - a.d] = s;
+    }
+    __syncthreads();
   }
 }
 
@@ -464,7 +469,7 @@ wavernn_status run_norm_grad(NormGradArgs& a, void* stream) {
   } else {
     a.parts = 0;
   }
-  if (wg && a.parts != 1) WR_LAUNCH(wr_norm_parts_kernel, (2 * (int64_t)a.d + 63) / 64, 1024, 0, stream, a);
+  if (wg && a.parts != 1) WR_LAUNCH(wr_norm_parts_kernel, std::min<int64_t>((2 * (int64_t)a.d + 63) / 64, WR_OP_BLOCKS), 1024, 0, stream, a);
   return WAVERNN_OK;
 }
 

@@ -116,3 +116,19 @@ def test_constant_rows_are_beta_wherever_they_lie(d):
         e = (depth(d) + 4) * U
         within(y, beta, e * e * x * 1e-5 ** -0.5 + 2 * U * beta.abs(), "y")
         within(mean, torch.full_like(mean, x), 2 * U * x, "mean")
+
+
+def whole(*shape, seed, dt=F32, most=3):
+    """Whole numbers -most .. most: sums of them are exact below 2^24."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randint(-most, most + 1, shape, generator=g, device="cuda", dtype=torch.int8).to(dt)
+
+
+@pytest.mark.parametrize("n", [0, 3])
+def test_weight_gradients_of_the_widest_rows(n):
+    """dgamma and dbeta of more than 2^27 columns, whose parts take more sums than a grid has room for."""
+    d = (1 << 27) + 5
+    x, dy = whole(n, d, seed=1, dt=BF16, most=1), whole(n, d, seed=2, dt=BF16)
+    mean, rstd = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda")
+    dx, dgamma, dbeta = ops.layer_norm_grad(dy, x, mean, rstd, out=dy.clone() if n else None)
+    assert torch.equal(dbeta, dy.sum(0, dtype=F32)) and torch.equal(dgamma, (dy * x).sum(0, dtype=F32))

@@ -17,8 +17,9 @@ import torch
 from . import wavernn as _w
 
 MAX_TOP = 32
-# (torch.cuda.current_stream() makes an object, which takes 2.6 us of a small call's 9)
-_raw_stream, _current_gpu = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# (torch.cuda.current_stream() makes an object, which takes 2.6 us of a small call's 9; a torch without GPU
+# support has neither, and no tensor that gets as far as them)
+_raw_stream, _current_gpu = (getattr(torch._C, k, None) for k in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
 _DTYPE = {torch.float32: _w.F32, torch.bfloat16: _w.BF16, torch.float16: _w.F16}
 _ID_BYTES = {torch.int32: 4, torch.int64: 8}
 

@@ -89,3 +89,15 @@ def test_score_tokens_checks_what_it_is_given(B, fused):
             m._check_scored(OnGpu(target), OnGpu(cond), {**ok, k: bad})
     m.cond_dim = 0                      # (a model without conditioning reads none)
     m._check_scored(OnGpu(target), cond, None)
+
+
+def test_the_operators_import_with_a_torch_without_gpu_support(monkeypatch):
+    import importlib.util
+    from paper_1802_08435_amd import ops
+    for k in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        monkeypatch.delattr(torch._C, k, raising=False)
+    spec = importlib.util.spec_from_file_location("paper_1802_08435_amd.ops_copy", ops.__file__)
+    copy = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(copy)
+    with pytest.raises(ValueError, match="GPU"):
+        copy.token_logprobs(torch.zeros(2, 4), torch.zeros(2, dtype=torch.int64))

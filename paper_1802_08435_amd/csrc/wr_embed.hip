@@ -76,8 +76,8 @@ __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
 // (slot 0: the chunk's beginning, slot 1: its end), and one more launch adds them
 // in chunk order.
 //
-// 16,384 bf16 rows of 1,024 into 50,021 fp32 (205 MB to write, 33 to read): 71 us, of it
-// the two passes with the clear 38, the sums 17, the frequent numbers' parts 8.
+// 16,384 bf16 rows of 1,024 into 50,021 fp32 (205 MB to write, 33 to read), uneven ids: 71 us a call among
+// others, of it the two passes with the clear 34 to 38, the sums 17, the frequent numbers' parts 8.
 #define SORT_THREADS 1024
 #define SORT_WAVES 16
 #define SORT_BITS 9
@@ -85,9 +85,13 @@ __global__ __launch_bounds__(256) void wr_embed_kernel(EmbedArgs a) {
 #define SORT_SMALL 4096
 #define SORT_TILE 2048
 #define SORT_TILES 256
-#define SORT_SELF 8        // (16,384 rows of 1,024 into 50,000: 68 us with counts, 63 so; 32,768: 36 and, so, 48)
+// Whole calls replayed in a graph, bf16 rows of 1,024 into 50,021 fp32: 16,384 even ids (8 tiles) 80.9 us with
+// counts, 78.0 so, uneven ones 75.2 and 73.7; 24,576 (12 tiles) 93.6 and 92.7, uneven 85.3 and 87.9; 32,768 (16) 95.8 and
+// 102.8.  Rows of 8, where the sort is most of the call: 24,576 41.0 and 43.9, 32,768 40.2 and 48.4.
+#define SORT_SELF 8
 #define EG_AHEAD 8
-#define EG_CHUNK_MIN 8      // positions of a chunk: doubled up to 64 while that leaves 1,024 blocks, four a CU (and 64 KiB of LDS are enough)
+#define EG_CHUNK_MIN 8      // positions of a chunk: doubled up to 64 while that leaves 1,024 blocks of a thread for four columns
+                            // (four a CU; half as many where a thread takes eight, with 16-bit types), and 64 KiB of LDS are enough
 #define EG_CHUNK_MAX 64
 #define EG_CLEAR 16384      // bytes that a block clears at a time
 #define EG_CLEAR_BLOCKS 512

@@ -406,8 +406,8 @@ __global__ __launch_bounds__(256) void wr_logp_rows_kernel(LogpArgs a) {
 // larger than the top-th largest logit, so only quads that reach it can hold an
 // alternative: their vectors (for few alternatives a small part of the row) are read once more,
 // from cache, and the classes that reach `low` are ranked among each other.
-// Bound by memory: 4,096 x 65,536 bf16 113 us without alternatives (4.7 TB/s, a copy's
-// rate), 127 with eight.
+// Bound by memory: 4,096 x 65,536 bf16 105 us without alternatives (5.1 TB/s; a copy reaches
+// 4.7), 122 with eight, each on its own; 145 in a training step, behind the gradient's 537 MB of writes.
 #define LW_U 4        // vectors in flight
 #define LW_CAP 1024   // classes ranked
 

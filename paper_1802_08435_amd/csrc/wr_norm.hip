@@ -14,10 +14,10 @@
 // or a block) with E vectors of 16 bytes each.  Blocks keep gamma and beta in registers and
 // take row after row; backward they also keep their columns' part of dgamma and dbeta,
 // which a second launch adds in the order of the blocks.  Rows past the widest
-// of these (2,048 vectors) are read from memory again for each sum (with 1,024 threads of four vectors
-// the registers spill: 1,024 x 20,000 bf16 75 us, 27 so; fp32 2,048 x 16,384 58 and 72).
-// 16,384 x 4,096 bf16 forward 47 us (5.7 TB/s), 16,384 x 2,048 backward 39 and 5 for the
-// parts (5.1 TB/s); a large copy 4.7.
+// of these (2,048 vectors) are read from memory again for each sum (with 1,024 threads of four vectors the
+// registers spill in 16 bits: 1,024 x 20,000 bf16 106 us, 25 so; fp32 2,048 x 16,384 66 and 82, 512 x 10,000 13.5 and 12.3).
+// 16,384 x 4,096 bf16 forward 48 us (5.6 TB/s), 16,384 x 2,048 backward 38 and 5 for the
+// parts (5.3 TB/s); a large copy 4.7.
 #include "wr_ops.h"
 
 namespace {
@@ -44,7 +44,7 @@ struct NormArgs {
 };
 
 // Sum over the wave's lanes of a row, in every one of them: within 16 lanes by rotations, which need no LDS and
-// pair the same operands as exchanges would (the second sum of the differences cost 1.2 us of 65,536 x 256 fp32 by those).
+// pair the same operands as exchanges would (65,536 x 256 fp32 forward 22.4 us, by exchanges 23.7).
 template <int N>
 __device__ __forceinline__ float rotate_add(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + N, 0xf, 0xf, true));
@@ -439,7 +439,8 @@ wavernn_status run_norm(NormArgs& a, void* stream) {
 
 // Parts of dgamma and dbeta of a call (dtype's bytes matter to the shape), a block each: one a CU where a
 // thread keeps 16 columns, two where fewer (20,000 x 257 fp32, 8 columns: 16.7 us with 512 parts, 20.0 with 256;
-// 20,000 x 768 bf16, 16 columns: 27.7 and 24.9, the parts being large), and two rows for each group of threads at least.
+// 20,000 x 768 bf16, 16 columns: 27.7 and 24.9, the parts being large), and two rows for each group of threads at
+// least (1,999 x 1,001 fp16, 125 parts, 12.9 us; with four rows 14.5, with one 12.4; 100 x 8,192 fp32 11.0, 13.0 and 11.7).
 int norm_parts(int64_t n, int32_t d, int bytes) {
   const int i = norm_shape(((int64_t)d * bytes + 15) / 16);
   const bool wide = i >= (int)(sizeof kShapes / sizeof kShapes[0]);
@@ -469,7 +470,8 @@ wavernn_status run_norm_grad(NormGradArgs& a, void* stream) {
   } else {
     a.parts = 0;
   }
-  if (wg && a.parts != 1) WR_LAUNCH(wr_norm_parts_kernel, std::min<int64_t>((2 * (int64_t)a.d + 63) / 64, WR_OP_BLOCKS), 1024, 0, stream, a);
+  if (wg && a.parts != 1)
+    WR_LAUNCH(wr_norm_parts_kernel, std::min<int64_t>((2 * (int64_t)a.d + 63) / 64, WR_OP_BLOCKS), 1024, 0, stream, a);
   return WAVERNN_OK;
 }
 

@@ -58,7 +58,7 @@ def _rows(name, t):
         if step is None:
             step = t.stride(d)
         elif t.stride(d) != step * run:
-            raise ValueError(f"{name}: the rows are not one distance apart")
+            raise ValueError(f"{name}: the rows are not one distance apart (take a contiguous copy, or the whole rows with padding)")
         run *= t.shape[d]
     return n, w, w if step is None else step
 
@@ -117,7 +117,9 @@ def token_logprobs(logits, tokens=None, top=0, stream=None):
     sum and the ``top`` most likely classes of every distribution: a dict of logp (None
     without tokens), entropy, lse [...], top_logp and top_idx [..., top] (None with top = 0), fp32 and
     int32.  tokens are int64 or int32; a negative one marks a row of padding, which is
-    not read and gives 0 (top_idx -1).  Masked classes are -inf.  Edge cases and the order of
+    not read and gives 0 (top_idx -1).  Masked classes are -inf.  Tokens one place ahead of their logits [B, T, V]
+    need no copy: give all T rows, with the tokens shifted and -1 in the last place (logits[:, :-1] is
+    refused, its rows being two distances apart).  Edge cases and the order of
     alternatives: include/wavernn.h, wavernn_token_logprobs."""
     if _away(logits, stream):
         return _there(token_logprobs, logits, stream, logits, tokens, top)
@@ -146,7 +148,8 @@ def token_logprobs_grad(logits, tokens, lse, entropy=None, g_logp=None, g_entrop
                         g_top=None, out=None, stream=None):
     """Gradient with respect to the logits of a loss whose gradients with respect to
     token_logprobs' results are g_logp, g_entropy, g_lse [...] and g_top [..., top] (of top_logp; any
-    may be None), given the results lse, entropy (for g_entropy) and top_idx (for g_top).
+    may be None), given the results lse, entropy (for g_entropy) and top_idx (for g_top).  The
+    probabilities are exp(logits - lse), as good as lse's fp32 rounding.
     ``out`` may be the logits themselves."""
     if _away(logits, stream):
         return _there(token_logprobs_grad, logits, stream, logits, tokens, lse, entropy, g_logp, g_entropy, g_lse, top_idx,
@@ -246,8 +249,8 @@ def layer_norm(x, gamma=None, beta=None, eps=1e-5, stats=False, out=None, stream
 
 def layer_norm_grad(dy, x, mean, rstd, gamma=None, weights=True, out=None, stream=None):
     """(dx, dgamma, dbeta) of layer_norm from dy [..., d], its x and the statistics it
-    returned; dx of x's dtype, dgamma and dbeta [d] float32 (None without ``weights``).  ``out``
-    (for dx) may be dy or x."""
+    returned; dx of x's dtype, dgamma and dbeta [d] float32 (None without ``weights``).  x - mean is as
+    good as mean's fp32 rounding.  ``out`` (for dx) may be dy or x."""
     if _away(x, stream):
         return _there(layer_norm_grad, x, stream, dy, x, mean, rstd, gamma, weights, out)
     L = _w._lib or _w.lib()

@@ -186,7 +186,9 @@ class Model:
             keep["_cnn"] = (ck, cc)
         h = ctypes.c_void_p()
         _check(L.wavernn_create(ctypes.byref(cfg), ctypes.byref(ws), ctypes.byref(h)))
+        import torch
         self._h = h
+        self.device = torch.device("cuda", torch.cuda.current_device())
         self.max_streams = max_streams
         self._front(w)
 
@@ -226,21 +228,25 @@ class Model:
 
     def _check_frames(self, name, x):
         import torch
-        if x.dim() != 3 or x.shape[2] != self.cond_dim or x.dtype != torch.float32 or not x.is_contiguous() or not x.is_cuda:
-            raise ValueError(f"{name} must be contiguous float32 [S][n_frames][{self.cond_dim}] on the GPU, "
+        dev = self.device
+        if x.dim() != 3 or x.shape[2] != self.cond_dim or x.dtype != torch.float32 or not x.is_contiguous() or x.device != dev:
+            raise ValueError(f"{name} must be contiguous float32 [S][n_frames][{self.cond_dim}] on the model's GPU, {dev}: "
                              f"got {x.dtype} {list(x.shape)} on {x.device}")
 
-    def _check_scored(self, target, cond, init):
-        """target, cond and init of a score_tokens call: the library gets addresses only."""
+    def _check_scored(self, target, cond, init, stream):
+        """Arguments of a score_tokens call: the library gets addresses only."""
         import torch
-        if target.dim() != 2 or target.dtype != torch.uint16 or not target.is_contiguous() or not target.is_cuda:
-            raise ValueError(f"target must be contiguous uint16 [S][T] on the GPU, got {target.dtype} {list(target.shape)} "
-                             f"on {target.device}")
-        S, dev = target.shape[0], target.device
+        dev = self.device
+        if target.dim() != 2 or target.dtype != torch.uint16 or not target.is_contiguous() or target.device != dev:
+            raise ValueError(f"target must be contiguous uint16 [S][T] on the model's GPU, {dev}: "
+                             f"got {target.dtype} {list(target.shape)} on {target.device}")
+        if stream is not None and stream.device != dev:
+            raise ValueError(f"the stream is on {stream.device}, the model on {dev}")
+        S = target.shape[0]
         if cond is not None and self.cond_dim > 0:
             self._check_frames("cond", cond)
-            if cond.shape[0] != S or cond.device != dev:
-                raise ValueError(f"cond holds {cond.shape[0]} utterances on {cond.device}, target {S} on {dev}")
+            if cond.shape[0] != S:
+                raise ValueError(f"cond holds {cond.shape[0]} utterances, target {S}")
         if init is not None:
             rows = S if self.fused else S * self.B
             for k, dtype, n in (("h", torch.float32, rows * self.H), ("c", torch.uint8, S * self.B), ("f", torch.uint8, S * self.B)):
@@ -401,15 +407,15 @@ class Model:
         low nibble of each) and, with top > 0, top_logp and top_idx [S][T][J][top] (else None).  The
         results belong to ``stream``, as ops' do."""
         import torch
-        self._check_scored(target, cond, init)
+        self._check_scored(target, cond, init, stream)
         S, T = target.shape
         J = 4 if self.fused else 2
         cond = self._cond(cond, labels, stream, S)
         k = max(int(top), 0)
         with torch.cuda.stream(stream):
-            logp, entropy = (torch.empty(S, T, J, device="cuda") for _ in range(2))
-            top_logp = torch.empty(S, T, J, k, device="cuda") if k else None
-            top_idx = torch.empty(S, T, J, k, dtype=torch.int32, device="cuda") if k else None
+            logp, entropy = (torch.empty(S, T, J, device=target.device) for _ in range(2))
+            top_logp = torch.empty(S, T, J, k, device=target.device) if k else None
+            top_idx = torch.empty(S, T, J, k, dtype=torch.int32, device=target.device) if k else None
         n_frames = 0 if cond is None else cond.shape[1]
         si = self._state(init)
         _check(lib().wavernn_score_tokens(self._h, S, T, _ptr(cond), n_frames, _ptr(target),

@@ -10,7 +10,7 @@ from paper_1802_08435_amd import wavernn as W  # noqa: E402
 
 def model(d=None, norm=False, fused=False, B=1):
     m = W.Model.__new__(W.Model)
-    m.H, m.B, m.cond_dim, m.fused, m._h = 64, B, 16, fused, None
+    m.H, m.B, m.cond_dim, m.fused, m._h, m.device = 64, B, 16, fused, None, torch.device("cuda", 0)
     m.E = None if d is None else torch.zeros(5, d)
     m.E_scale, m.ln_eps = 1.0, 1e-5
     m.ln_g, m.ln_b = (torch.ones(16), torch.zeros(16)) if norm else (None, None)
@@ -22,7 +22,7 @@ def test_features_on_the_cpu(norm):
     """Without a layer norm they are the frames as they are, and only their address goes on."""
     m, x = model(norm=norm), torch.zeros(2, 7, 16)
     for call in (lambda: m.frames(x), lambda: m.sample(100, labels=x, n_streams=2), lambda: m.frames_grad(x, x)):
-        with pytest.raises(ValueError, match="on the GPU"):
+        with pytest.raises(ValueError, match="on the model's GPU"):
             call()
 
 
@@ -69,26 +69,32 @@ def test_score_tokens_checks_what_it_is_given(B, fused):
     target, cond = torch.zeros(S, 100, dtype=torch.uint16), torch.zeros(S, 3, 16)
     init = dict(h=torch.zeros(rows, 64), c=torch.zeros(S * B, dtype=torch.uint8), f=torch.zeros(S * B, dtype=torch.uint8))
     ok = {k: OnGpu(t) for k, t in init.items()}
-    m._check_scored(OnGpu(target), OnGpu(cond), ok)
-    m._check_scored(OnGpu(target[:, :0]), OnGpu(cond), None)
-    m._check_scored(OnGpu(target), None, None)
-    for bad in (target, OnGpu(target.to(torch.int32)), OnGpu(target.view(-1)), OnGpu(target[:, ::2])):
+    m._check_scored(OnGpu(target), OnGpu(cond), ok, None)
+    m._check_scored(OnGpu(target[:, :0]), OnGpu(cond), None, None)
+    m._check_scored(OnGpu(target), None, None, None)
+    for bad in (target, OnGpu(target, 1), OnGpu(target.to(torch.int32)), OnGpu(target.view(-1)), OnGpu(target[:, ::2])):
         with pytest.raises(ValueError, match="target must be"):
-            m._check_scored(bad, OnGpu(cond), None)
+            m._check_scored(bad, OnGpu(cond), None, None)
     with pytest.raises(ValueError, match="target must be"):
         m.score_tokens(target)
-    for bad in (cond, OnGpu(cond.half()), OnGpu(cond[:, :, :8].contiguous()), OnGpu(cond.transpose(0, 1)), OnGpu(cond[0])):
+
+    class Away:
+        device = torch.device("cuda", 1)
+
+    with pytest.raises(ValueError, match="the stream is on"):
+        m._check_scored(OnGpu(target), None, None, Away())
+    for bad in (cond, OnGpu(cond.half()), OnGpu(cond[:, :, :8].contiguous()), OnGpu(cond.transpose(0, 1)), OnGpu(cond[0]),
+                OnGpu(cond, 1)):
         with pytest.raises(ValueError, match="cond must be"):
-            m._check_scored(OnGpu(target), bad, None)
-    for bad in (OnGpu(cond[:1]), OnGpu(cond, 1)):
-        with pytest.raises(ValueError, match="cond holds"):
-            m._check_scored(OnGpu(target), bad, None)
+            m._check_scored(OnGpu(target), bad, None, None)
+    with pytest.raises(ValueError, match="cond holds"):
+        m._check_scored(OnGpu(target), OnGpu(cond[:1]), None, None)
     for k, bad in (("h", init["h"]), ("h", OnGpu(init["h"][1:])), ("h", OnGpu(init["h"].double())), ("c", OnGpu(init["c"][1:])),
                    ("c", OnGpu(init["c"].int())), ("f", OnGpu(init["f"], 1)), ("f", OnGpu(init["f"][:1].expand(2 * B)))):
         with pytest.raises(ValueError, match="init's " + k):
-            m._check_scored(OnGpu(target), OnGpu(cond), {**ok, k: bad})
+            m._check_scored(OnGpu(target), OnGpu(cond), {**ok, k: bad}, None)
     m.cond_dim = 0                      # (a model without conditioning reads none)
-    m._check_scored(OnGpu(target), cond, None)
+    m._check_scored(OnGpu(target), cond, None, None)
 
 
 def test_the_operators_import_with_a_torch_without_gpu_support(monkeypatch):

@@ -77,8 +77,8 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float* s) {
 
 // 1 / sqrt(variance + eps) from the mean square and the mean of the differences.
 __device__ __forceinline__ float norm_rstd(float square, float dm, float eps) {
-  const float v = square - dm * dm;
-  return 1.0f / sqrtf((v < 0.0f ? 0.0f : v) + eps);   // (a NaN stays)
+  const float v = square - (square > 3.0e38f ? 0.0f : dm * dm);   // (past fp32's range both may be infinite)
+  return 1.0f / sqrtf((v < 0.0f ? 0.0f : v) + eps);               // (a NaN stays)
 }
 
 // Columns of thread t's vector e: where it begins, how many of its first elements are not its own

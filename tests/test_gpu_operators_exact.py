@@ -351,3 +351,12 @@ def test_layer_norm_gradient_without_some_of_its_results(n, d, dt):
                                            rstd.data_ptr(), _addr(out.get("dx")), d, _addr(out.get("dgamma")),
                                            _addr(out.get("dbeta")), ws.data_ptr(), size, st))
         assert all(torch.equal(out[k], want[k]) for k in use), use
+
+
+@pytest.mark.parametrize("d", [64, 1000, 9000])
+def test_rows_whose_variance_overflows_are_beta(d):
+    """Spreads past fp32's range (finite sums): 1 / sqrt(inf) leaves beta, whatever is left of the mean."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    x, beta = 1e33 * torch.randn(3, d, generator=g, device="cuda"), torch.arange(float(d), device="cuda")
+    y, mean, rstd = ops.layer_norm(x, None, beta, stats=True)
+    assert torch.equal(y, beta.expand(3, d)) and torch.equal(rstd, torch.zeros(3, device="cuda"))
